@@ -1,7 +1,8 @@
 /*
  * resist_ops.h -- layer-level entry points of the same library: the convolution kernels that
  * resist_local_step is built from, exposed so each can be checked against the textbook
- * definition on its own.  Same conventions as resist.h (status codes, caller-owned device
+ * definition on its own; and, further down, the operators of residual blocks of dense layers (layer
+ * norm, dropout, dense layers with their epilogue).  Same conventions as resist.h (status codes, caller-owned device
  * memory, caller's stream, no synchronisation).
  *
  * Layouts: activations NHWC [N][H][W][C]; filters [K][R][S][C]; outputs [N][P][Q][K] with
@@ -79,6 +80,104 @@ int resist_stem_conv2d_wgrad(const resist_conv_shape *s, const void *dy, const f
 int resist_conv2d_wgrad_static(const resist_conv_shape *s, const void *dy, const void *x, float *dw,
                                void *hip_stream);
 int resist_conv2d_wgrad_static_limit(int64_t *bytes);
+
+/*
+ * Operators of a residual block of dense layers:
+ *     n = layernorm(x);   h = dropout(act(n w1' + b1));   y = x + dropout(h w2' + b2)
+ * and their gradients.  Same conventions; in particular every pointer is 16-byte aligned.  Rows are tokens: a matrix is M rows of
+ * contiguous elements, `ld` elements from one row to the next (at least the row's length; 0: exactly that).  Activations, their
+ * gradients and the weights w [N][K] (dense) are dtype 0 fp32 or 1 bf16; biases, LN parameters and statistics, and the
+ * gradients of parameters are fp32.  All arithmetic is fp32 (products of fp32 operands as under compute_dtype in resist.h), with one
+ * rounding where a result is stored.  M may be 0: nothing is written but the gradients of parameters, which are zero.  An output
+ * may be the very tensor (pointer and stride) that it is named after with "in place" below; otherwise outputs overlap nothing.
+ *
+ * Activations `act`:
+ *   RESIST_ACT_NONE       a(z) = z
+ *   RESIST_ACT_RELU       max(z, 0), with a'(0) = 0
+ *   RESIST_ACT_GELU       z Phi(z), Phi the normal distribution function
+ *   RESIST_ACT_GELU_TANH  z/2 (1 + tanh(sqrt(2/pi) (z + 0.044715 z^3)))
+ *   RESIST_ACT_SILU       z / (1 + exp(-z))
+ *
+ * Dropout with probability 0 <= p < 1: an element is dropped (0, whatever it was) or kept and multiplied by 1/(1-p).  The mask is never
+ * stored: it is a function of rng, device {seed, offset}, read when the kernel runs (a captured call draws a new mask with
+ * every replay if the caller moves the offset on in between), and of the position.  With splitmix64 as in
+ * resist_partition, let s be the first output of the sequence seeded with `seed`, and word(i, c) output number
+ * offset + i*ceil(N/2) + c (from 0) of the sequence seeded with s.  Element (i, j) of an M x N matrix is dropped where the low (j even)
+ * or high (j odd) 32 bits of word(i, j/2) are below p 2^32, rounded to a whole number.  So a call uses M*ceil(N/2) words: a
+ * caller who wants independent masks moves the offset on by that.  The same rng, p, M and N give the same mask in every call
+ * below.  rng may be NULL where p is 0.
+ */
+enum { RESIST_ACT_NONE = 0, RESIST_ACT_RELU = 1, RESIST_ACT_GELU = 2, RESIST_ACT_GELU_TANH = 3, RESIST_ACT_SILU = 4 };
+
+/*
+ * Layer norm over rows of N elements (1 <= N <= 2^24, M < 2^31):
+ *   forward   mu = mean x, v = mean (x - mu)^2, r = 1/sqrt(v + eps);  y = gamma (x - mu) r + beta      [y in place of x]
+ *   backward  xhat = (x - mu) r, g = gamma dy;  dx = r (g - mean g - xhat mean(g xhat)) [+ addend]     [dx in place of dy, x or addend]
+ *             dgamma = sum over rows of dy xhat, dbeta = sum over rows of dy
+ *   gamma, beta    device [N] or NULL (1, 0)          eps  >= 0
+ *   mean, rstd     device [M]: mu and r, written by the forward pass (or NULL), read by the backward pass
+ *   addend         device [M][N] or NULL: a gradient that reaches x by another path
+ *   dgamma, dbeta  device [N] or NULL
+ *   workspace      resist_layernorm_workspace_bytes (backward only): partial sums; calls that overlap in time need one each
+ */
+int resist_layernorm_workspace_bytes(int64_t M, int32_t N, int64_t *bytes);
+int resist_layernorm_forward(int64_t M, int32_t N, int32_t dtype, const void *x, int64_t ldx, const float *gamma, const float *beta,
+                             float eps, void *y, int64_t ldy, float *mean, float *rstd, void *hip_stream);
+int resist_layernorm_backward(int64_t M, int32_t N, int32_t dtype, const void *dy, int64_t lddy, const void *x, int64_t ldx,
+                              const float *gamma, const float *mean, const float *rstd, const void *addend, int64_t ldadd, void *dx,
+                              int64_t lddx, float *dgamma, float *dbeta, void *workspace, int64_t workspace_bytes, void *hip_stream);
+
+/*
+ * Dropout on its own, with the residual add behind it, and its gradient, with that of an activation in front of it
+ * (1 <= N <= 2^24, M < 2^31):
+ *   forward   y = [residual +] drop(x)       [y in place of x or residual]
+ *   backward  dx = a'(z) drop(dy)            [dx in place of dy or z]       (act RESIST_ACT_NONE: z is not read)
+ */
+int resist_dropout_forward(int64_t M, int32_t N, int32_t dtype, const void *x, int64_t ldx, double p, const uint64_t *rng,
+                           const void *residual, int64_t ldr, void *y, int64_t ldy, void *hip_stream);
+int resist_dropout_backward(int64_t M, int32_t N, int32_t dtype, const void *dy, int64_t lddy, double p, const uint64_t *rng, int32_t act,
+                            const void *z, int64_t ldz, void *dx, int64_t lddx, void *hip_stream);
+
+/*
+ * Dense layer, x [M][K], w [N][K], y [M][N] (1 <= K, N <= 2^20, row strides up to 2^20, M < 2^31):
+ *   forward          z = x w' + bias,  y = [residual +] drop(act(z))      [y in place of residual]
+ *   data gradient    dx = a'(z) drop(dz w): z, act and drop are of the layer that produced x, the gradient leaves taken
+ *                    through them                                         [dx in place of z]
+ *   weight gradient  dw = dz' x [N][K], db = column sums of dz [N]; either may be NULL
+ * dz and y share ldy, dx and x share ldx.
+ * Workspace (may be NULL where resist_linear_workspace_bytes is 0): operands laid out for the kernels, and partial sums; calls
+ * that overlap in time need one each.  op: 0 forward, 1 data gradient, 2 weight gradient.  It depends on the shape alone.
+ */
+typedef struct {
+  int64_t M;
+  int32_t K, N;
+  int64_t ldx, ldy;
+  int32_t dtype;
+} resist_linear_shape;
+typedef struct {
+  const float *bias;        /* device [N] or NULL */
+  int32_t act;
+  double p;                 /* dropout; rng device [2] */
+  const uint64_t *rng;
+  const void *residual;     /* device [M][N] or NULL */
+  int64_t ldr;
+  void *z;                  /* device [M][N] or NULL: receives z, as the gradients need it */
+  int64_t ldz;
+} resist_linear_epilogue;
+typedef struct {
+  int32_t act;              /* RESIST_ACT_NONE: z is not read */
+  const void *z;            /* device [M][K] */
+  int64_t ldz;
+  double p;
+  const uint64_t *rng;
+} resist_linear_through;
+int resist_linear_workspace_bytes(const resist_linear_shape *s, int32_t op, int64_t *bytes);
+int resist_linear_forward(const resist_linear_shape *s, const void *x, const void *w, const resist_linear_epilogue *epilogue /* or NULL */,
+                          void *y, void *workspace, int64_t workspace_bytes, void *hip_stream);
+int resist_linear_dgrad(const resist_linear_shape *s, const void *dz, const void *w, const resist_linear_through *through /* or NULL */,
+                        void *dx, void *workspace, int64_t workspace_bytes, void *hip_stream);
+int resist_linear_wgrad(const resist_linear_shape *s, const void *dz, const void *x, float *dw, float *db, void *workspace,
+                        int64_t workspace_bytes, void *hip_stream);
 
 #ifdef __cplusplus
 }

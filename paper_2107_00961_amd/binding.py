@@ -30,6 +30,19 @@ class _KernelStat(C.Structure):
                 ("flops", C.c_double), ("bytes", C.c_double)]
 
 
+class _LinearShape(C.Structure):
+    _fields_ = [("M", C.c_int64), ("K", C.c_int32), ("N", C.c_int32), ("ldx", C.c_int64), ("ldy", C.c_int64), ("dtype", C.c_int32)]
+
+
+class _LinearEpilogue(C.Structure):
+    _fields_ = [("bias", C.c_void_p), ("act", C.c_int32), ("p", C.c_double), ("rng", C.c_void_p), ("residual", C.c_void_p),
+                ("ldr", C.c_int64), ("z", C.c_void_p), ("ldz", C.c_int64)]
+
+
+class _LinearThrough(C.Structure):
+    _fields_ = [("act", C.c_int32), ("z", C.c_void_p), ("ldz", C.c_int64), ("p", C.c_double), ("rng", C.c_void_p)]
+
+
 class _ConvShape(C.Structure):
     _fields_ = [(n, C.c_int32) for n in ("N", "H", "W", "C", "K", "R", "S", "stride", "pad", "dtype")]
 
@@ -88,6 +101,16 @@ def lib():
             getattr(L, name).argtypes = [C.POINTER(_ConvShape), C.c_void_p, C.c_void_p, C.c_void_p,
                                          C.c_void_p, C.c_int64, C.c_void_p]
         L.resist_conv2d_wgrad_static.argtypes = [C.POINTER(_ConvShape), C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p]
+        vp, i32, i64 = C.c_void_p, C.c_int32, C.c_int64
+        L.resist_layernorm_workspace_bytes.argtypes = [i64, i32, C.POINTER(i64)]
+        L.resist_layernorm_forward.argtypes = [i64, i32, i32, vp, i64, vp, vp, C.c_float, vp, i64, vp, vp, vp]
+        L.resist_layernorm_backward.argtypes = [i64, i32, i32, vp, i64, vp, i64, vp, vp, vp, vp, i64, vp, i64, vp, vp, vp, i64, vp]
+        L.resist_dropout_forward.argtypes = [i64, i32, i32, vp, i64, C.c_double, vp, vp, i64, vp, i64, vp]
+        L.resist_dropout_backward.argtypes = [i64, i32, i32, vp, i64, C.c_double, vp, i32, vp, i64, vp, i64, vp]
+        L.resist_linear_workspace_bytes.argtypes = [C.POINTER(_LinearShape), i32, C.POINTER(i64)]
+        L.resist_linear_forward.argtypes = [C.POINTER(_LinearShape), vp, vp, C.POINTER(_LinearEpilogue), vp, vp, i64, vp]
+        L.resist_linear_dgrad.argtypes = [C.POINTER(_LinearShape), vp, vp, C.POINTER(_LinearThrough), vp, vp, i64, vp]
+        L.resist_linear_wgrad.argtypes = [C.POINTER(_LinearShape), vp, vp, vp, vp, vp, i64, vp]
         _lib = L
     return _lib
 
@@ -449,3 +472,253 @@ def stem_conv2d_wgrad(dy, x, w_shape, stride, pad, stream=None):
     _check(lib().resist_stem_conv2d_wgrad(C.byref(sh), dy.data_ptr(), x.data_ptr(), dw.data_ptr(), ws.data_ptr(), ws.numel(),
                                           _stream_ptr(stream)))
     return dw
+
+
+# ---- operators of a dense residual block ---------------------------------------------------------------------------
+# Matrices are two-dimensional tensors [rows, N].  Their rows may be apart (a slice of a wider matrix); one whose rows are not
+# contiguous or not 16-byte aligned at the start is copied first.  Results are new tensors on the stream the call runs on (the
+# current one, or `stream`).
+ACTIVATIONS = {"none": 0, "relu": 1, "gelu": 2, "gelu_tanh": 3, "silu": 4}
+
+
+class _On:
+    """The device of the call's tensors as the current device, and its stream (hipStream_t in .ptr); results and workspaces are
+    allocated for that stream."""
+
+    def __init__(self, tensor, stream):
+        import torch
+        if not tensor.is_cuda:
+            raise ResistError("device tensors only: there is no CPU path")
+        if stream is not None and stream.device != tensor.device:
+            raise ResistError(f"a stream of {stream.device} for tensors on {tensor.device}")
+        self._guards = []
+        if tensor.device.index != torch.cuda.current_device():
+            self._guards.append(torch.cuda.device(tensor.device))
+        if stream is not None:
+            self._guards.append(torch.cuda.stream(stream))
+        self._torch, self._stream, self.device = torch, stream, tensor.device
+
+    def __enter__(self):
+        for g in self._guards:
+            g.__enter__()
+        self.ptr = (self._stream or self._torch.cuda.current_stream()).cuda_stream
+        return self
+
+    def __exit__(self, *exc):
+        for g in reversed(self._guards):
+            g.__exit__(*exc)
+
+    def uses(self, *tensors):
+        """The call's inputs: memory of theirs that is given back meanwhile waits for a stream that is not their own."""
+        if self._stream is not None:
+            for t in tensors:
+                if t is not None:
+                    t.record_stream(self._stream)
+
+
+def _matrix(t, what, like=None, shape=None):
+    """t as rows the library takes; checked against the call's first tensor."""
+    if t.dim() != 2:
+        raise ResistError(f"{what}: a matrix [rows, N] is needed, got {tuple(t.shape)}")
+    if like is not None and (t.dtype != like.dtype or t.device != like.device):
+        raise ResistError(f"{what}: {t.dtype} on {t.device} beside {like.dtype} on {like.device}")
+    if shape is not None and tuple(t.shape) != tuple(shape):
+        raise ResistError(f"{what}: shape {tuple(t.shape)} where {tuple(shape)} is needed")
+    if t.shape[1] == 0:
+        raise ResistError(f"{what}: rows without elements")
+    if t.stride(1) != 1 and t.shape[1] > 1 or t.stride(0) < t.shape[1] and t.shape[0] > 1 or t.data_ptr() % 16:
+        import torch
+        t = t.clone(memory_format=torch.contiguous_format)
+    return t
+
+
+def _ld(t):
+    """Row stride for the library: 0 (dense) where there is no second row to say it."""
+    return t.stride(0) if t.shape[0] > 1 else 0
+
+
+def _vector(t, what, n, like):
+    """A parameter vector [n] float32, or None -> itself, contiguous and aligned."""
+    import torch
+    if t is None:
+        return None
+    if t.dtype != torch.float32 or t.device != like.device or tuple(t.shape) != (n,):
+        raise ResistError(f"{what}: float32 [{n}] on {like.device} is needed, got {t.dtype} {tuple(t.shape)} on {t.device}")
+    return t if t.is_contiguous() and t.data_ptr() % 16 == 0 else t.clone(memory_format=torch.contiguous_format)
+
+
+def _rng_ptr(rng, p, like):
+    """{seed, offset}: a device tensor of two 64-bit integers, read when the kernel runs."""
+    import torch
+    if rng is None:
+        if p:
+            raise ResistError("rng: needed where p is not 0")
+        return None
+    if rng.dtype not in (torch.int64, torch.uint64) or rng.device != like.device or tuple(rng.shape) != (2,) or not rng.is_contiguous():
+        raise ResistError(f"rng: two contiguous 64-bit integers on {like.device} are needed")
+    return rng.data_ptr()
+
+
+def _activation(act):
+    if act not in ACTIVATIONS:
+        raise ResistError(f"act {act!r}: one of {', '.join(ACTIVATIONS)}")
+    return ACTIVATIONS[act]
+
+
+def _opt(t):
+    return t.data_ptr() if t is not None else None
+
+
+def layernorm_forward(x, gamma=None, beta=None, eps=1e-5, stream=None):
+    """x [M, N] float32 or bfloat16; gamma, beta [N] float32 or None -> (y, mean [M], rstd [M])."""
+    import torch
+    with _On(x, stream) as on:
+        dt = _dtype_code(x)
+        x = _matrix(x, "x")
+        M, N = x.shape
+        gamma, beta = _vector(gamma, "gamma", N, x), _vector(beta, "beta", N, x)
+        on.uses(x, gamma, beta)
+        y = torch.empty((M, N), dtype=x.dtype, device=on.device)
+        mean = torch.empty(M, dtype=torch.float32, device=on.device)
+        rstd = torch.empty(M, dtype=torch.float32, device=on.device)
+        _check(lib().resist_layernorm_forward(M, N, dt, x.data_ptr(), _ld(x), _opt(gamma), _opt(beta), eps, y.data_ptr(), 0,
+                                              mean.data_ptr(), rstd.data_ptr(), on.ptr))
+    return y, mean, rstd
+
+
+def layernorm_backward(dy, x, gamma, mean, rstd, addend=None, stream=None):
+    """Gradients of layernorm_forward: dy, x [M, N], gamma [N] or None, mean and rstd as it returned them; addend [M, N] or None is
+    added to dx -> (dx, dgamma [N], dbeta [N])."""
+    import torch
+    with _On(x, stream) as on:
+        dt = _dtype_code(x)
+        x = _matrix(x, "x")
+        M, N = x.shape
+        dy = _matrix(dy, "dy", x, (M, N))
+        addend = _matrix(addend, "addend", x, (M, N)) if addend is not None else None
+        gamma = _vector(gamma, "gamma", N, x)
+        if mean is None or rstd is None:
+            raise ResistError("mean and rstd: those of layernorm_forward are needed")
+        mean, rstd = _vector(mean, "mean", M, x), _vector(rstd, "rstd", M, x)
+        on.uses(dy, x, gamma, mean, rstd, addend)
+        dx = torch.empty((M, N), dtype=x.dtype, device=on.device)
+        dparams = torch.empty((2, (N + 3) // 4 * 4), dtype=torch.float32, device=on.device)
+        n = C.c_int64()
+        _check(lib().resist_layernorm_workspace_bytes(M, N, C.byref(n)))
+        ws = torch.empty(n.value, dtype=torch.uint8, device=on.device)
+        dgamma, dbeta = dparams[0, :N], dparams[1, :N]
+        _check(lib().resist_layernorm_backward(M, N, dt, dy.data_ptr(), _ld(dy), x.data_ptr(), _ld(x), _opt(gamma), mean.data_ptr(),
+                                               rstd.data_ptr(), _opt(addend), _ld(addend) if addend is not None else 0, dx.data_ptr(), 0,
+                                               dgamma.data_ptr(), dbeta.data_ptr(), ws.data_ptr(), n.value, on.ptr))
+    return dx, dgamma, dbeta
+
+
+def dropout_forward(x, p, rng, residual=None, stream=None):
+    """[residual +] dropout(x), x [M, N]: elements dropped with probability p, the others times 1/(1-p).  rng: device tensor of two 64-bit
+    integers {seed, offset}; a call uses M * ceil(N/2) numbers from `offset` on, the same rng, p and shape give the same mask."""
+    import torch
+    with _On(x, stream) as on:
+        dt = _dtype_code(x)
+        x = _matrix(x, "x")
+        M, N = x.shape
+        residual = _matrix(residual, "residual", x, (M, N)) if residual is not None else None
+        on.uses(x, rng, residual)
+        y = torch.empty((M, N), dtype=x.dtype, device=on.device)
+        _check(lib().resist_dropout_forward(M, N, dt, x.data_ptr(), _ld(x), p, _rng_ptr(rng, p, x), _opt(residual),
+                                            _ld(residual) if residual is not None else 0, y.data_ptr(), 0, on.ptr))
+    return y
+
+
+def dropout_backward(dy, p, rng, act="none", z=None, stream=None):
+    """Gradient of dropout(act(z)) with respect to z [M, N] from dy [M, N] (act "none": of dropout alone, z is not read)."""
+    import torch
+    with _On(dy, stream) as on:
+        dt, code = _dtype_code(dy), _activation(act)
+        dy = _matrix(dy, "dy")
+        M, N = dy.shape
+        if code and z is None:
+            raise ResistError("z: needed for the gradient of an activation")
+        z = _matrix(z, "z", dy, (M, N)) if code else None
+        on.uses(dy, rng, z)
+        dx = torch.empty((M, N), dtype=dy.dtype, device=on.device)
+        _check(lib().resist_dropout_backward(M, N, dt, dy.data_ptr(), _ld(dy), p, _rng_ptr(rng, p, dy), code, _opt(z),
+                                             _ld(z) if z is not None else 0, dx.data_ptr(), 0, on.ptr))
+    return dx
+
+
+def _linear_ws(shape, op, device):
+    import torch
+    n = C.c_int64()
+    _check(lib().resist_linear_workspace_bytes(C.byref(shape), op, C.byref(n)))
+    return (torch.empty(n.value, dtype=torch.uint8, device=device) if n.value else None), n.value
+
+
+def _weights(w, like, K=None, N=None):
+    if w.dim() != 2 or K is not None and w.shape[1] != K or N is not None and w.shape[0] != N or w.shape[0] < 1:
+        raise ResistError(f"w: [N, K] is needed, got {tuple(w.shape)} beside {tuple(like.shape)}")
+    w = _matrix(w, "w", like)
+    return w if w.is_contiguous() else w.contiguous()
+
+
+def linear_forward(x, w, bias=None, act="none", p=0.0, rng=None, residual=None, keep_z=False, stream=None):
+    """[residual +] dropout(act(x w' + bias)): x [M, K] and w [N, K] of one dtype, bias [N] float32 or None, residual [M, N] or None;
+    dropout as in dropout_forward -> y [M, N], with keep_z (y, z), z = x w' + bias as the gradients need it."""
+    import torch
+    with _On(x, stream) as on:
+        dt, code = _dtype_code(x), _activation(act)
+        x = _matrix(x, "x")
+        M, K = x.shape
+        w = _weights(w, x, K=K)
+        N = w.shape[0]
+        bias = _vector(bias, "bias", N, x)
+        residual = _matrix(residual, "residual", x, (M, N)) if residual is not None else None
+        on.uses(x, w, bias, rng, residual)
+        y = torch.empty((M, N), dtype=x.dtype, device=on.device)
+        z = torch.empty((M, N), dtype=x.dtype, device=on.device) if keep_z else None
+        sh = _LinearShape(M, K, N, _ld(x), 0, dt)
+        e = _LinearEpilogue(_opt(bias), code, p, _rng_ptr(rng, p, x), _opt(residual), _ld(residual) if residual is not None else 0, _opt(z), 0)
+        ws, n = _linear_ws(sh, 0, on.device)
+        _check(lib().resist_linear_forward(C.byref(sh), x.data_ptr(), w.data_ptr(), C.byref(e), y.data_ptr(), _opt(ws), n, on.ptr))
+    return (y, z) if keep_z else y
+
+
+def linear_dgrad(dz, w, act="none", z=None, p=0.0, rng=None, stream=None):
+    """Gradient with respect to the input of a dense layer, dz w, dz [M, N], w [N, K] -- taken on, where that input was dropout(act(z)) with
+    z [M, K], through this dropout and activation to the gradient with respect to z."""
+    import torch
+    with _On(dz, stream) as on:
+        dt, code = _dtype_code(dz), _activation(act)
+        dz = _matrix(dz, "dz")
+        M, N = dz.shape
+        w = _weights(w, dz, N=N)
+        K = w.shape[1]
+        if code and z is None:
+            raise ResistError("z: needed for the gradient of an activation")
+        z = _matrix(z, "z", dz, (M, K)) if code else None
+        on.uses(dz, w, z, rng)
+        dx = torch.empty((M, K), dtype=dz.dtype, device=on.device)
+        sh = _LinearShape(M, K, N, 0, _ld(dz), dt)
+        t = _LinearThrough(code, _opt(z), _ld(z) if z is not None else 0, p, _rng_ptr(rng, p, dz))
+        ws, n = _linear_ws(sh, 1, on.device)
+        _check(lib().resist_linear_dgrad(C.byref(sh), dz.data_ptr(), w.data_ptr(), C.byref(t), dx.data_ptr(), _opt(ws), n, on.ptr))
+    return dx
+
+
+def linear_wgrad(dz, x, stream=None):
+    """Gradients of a dense layer's parameters: dz [M, N], x [M, K] -> (dw [N, K], db [N]), float32."""
+    import torch
+    with _On(x, stream) as on:
+        dt = _dtype_code(x)
+        x = _matrix(x, "x")
+        M, K = x.shape
+        dz = _matrix(dz, "dz", x)
+        if dz.shape[0] != M:
+            raise ResistError(f"dz: {dz.shape[0]} rows beside {M} of x")
+        N = dz.shape[1]
+        on.uses(dz, x)
+        dw = torch.empty((N, K), dtype=torch.float32, device=on.device)
+        db = torch.empty(N, dtype=torch.float32, device=on.device)
+        sh = _LinearShape(M, K, N, _ld(x), _ld(dz), dt)
+        ws, n = _linear_ws(sh, 2, on.device)
+        _check(lib().resist_linear_wgrad(C.byref(sh), dz.data_ptr(), x.data_ptr(), dw.data_ptr(), db.data_ptr(), _opt(ws), n, on.ptr))
+    return dw, db

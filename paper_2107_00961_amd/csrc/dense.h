@@ -1,0 +1,135 @@
+// What the kernels of a dense residual block (layernorm.hip, dropout.hip, linear.hip) share: access to rows that start anywhere, the
+// dropout generator, the activations and their derivatives.
+#pragma once
+#include <math.h>
+
+#include "elem.h"
+#include "internal.h"
+
+namespace resist {
+
+// Rows of a matrix whose stride or width is no multiple of 16 bytes start anywhere an element can: 16-byte accesses that promise no more
+// than the element's own alignment (one instruction each all the same: global memory takes any address).
+typedef f32x4 f32x4_any __attribute__((aligned(4)));
+typedef u32x4 u32x4_any __attribute__((aligned(2)));
+template <typename T> struct Row;
+template <> struct Row<float> {
+  __device__ static inline void load(const float *p, float (&v)[8]) {
+    const f32x4 a = *reinterpret_cast<const f32x4_any *>(p), b = *reinterpret_cast<const f32x4_any *>(p + 4);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) { v[e] = a[e]; v[e + 4] = b[e]; }
+  }
+  __device__ static inline void store(float *p, const float (&v)[8]) {
+    *reinterpret_cast<f32x4_any *>(p) = f32x4{v[0], v[1], v[2], v[3]};
+    *reinterpret_cast<f32x4_any *>(p + 4) = f32x4{v[4], v[5], v[6], v[7]};
+  }
+};
+template <> struct Row<__bf16> {
+  __device__ static inline void load(const __bf16 *p, float (&v)[8]) {
+    const u32x4 t = *reinterpret_cast<const u32x4_any *>(p);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) { v[2 * i] = bf16_lo(t[i]); v[2 * i + 1] = bf16_hi(t[i]); }
+  }
+  __device__ static inline void store(__bf16 *p, const float (&v)[8]) {
+    u32x4 t;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) t[i] = pack_bf16x2(v[2 * i], v[2 * i + 1]);
+    *reinterpret_cast<u32x4_any *>(p) = t;
+  }
+};
+// eight elements of a row, or the `left` < 8 that it still has (the others read as zero, and are not written)
+template <typename T> __device__ inline void row_load(const T *p, int left, float (&v)[8]) {
+  if (left >= 8) { Row<T>::load(p, v); return; }
+#pragma unroll
+  for (int e = 0; e < 8; ++e) v[e] = e < left ? (float)p[e] : 0.f;
+}
+template <typename T> __device__ inline void row_store(T *p, int left, const float (&v)[8]) {
+  if (left >= 8) { Row<T>::store(p, v); return; }
+#pragma unroll
+  for (int e = 0; e < 8; ++e)
+    if (e < left) p[e] = (T)v[e];
+}
+
+// ---- dropout: splitmix64 addressed by position.  Output number c of the sequence started from `state` is a pure function of
+// state + (c + 1) * golden, so the mask is computed wherever it is needed and never stored.  state is itself the
+// first output of the sequence seeded with the caller's seed: sequences of neighbouring seeds would else be the same one, shifted.
+typedef unsigned long long u64;
+constexpr u64 kGolden = 0x9E3779B97F4A7C15ull;
+__device__ inline u64 splitmix(u64 z) {
+  z = (z ^ (z >> 30)) * 0xBF58476D1CE4E5B9ull;
+  z = (z ^ (z >> 27)) * 0x94D049BB133111EBull;
+  return z ^ (z >> 31);
+}
+struct Dropout {
+  const u64 *rng;   // device {seed, offset}; NULL: every element is kept
+  unsigned thr;     // an element is dropped where its 32 bits are below p * 2^32
+  float scale;      // 1 / (1 - p)
+};
+inline Dropout make_dropout(const DropSpec &s) {
+  if (s.p == 0. || !s.rng) return Dropout{nullptr, 0, 1.f};
+  return Dropout{reinterpret_cast<const u64 *>(s.rng), (unsigned)nearbyint(s.p * 4294967296.), (float)(1. / (1. - s.p))};
+}
+// what a word's number is added to: word c is splitmix(base + c * golden)
+__device__ inline u64 dropout_base(const u64 *rng) { return splitmix(rng[0] + kGolden) + (rng[1] + 1) * kGolden; }
+// elements j .. j+7 of a row (j even) whose first word is number `word`
+__device__ inline void dropout8(u64 base, u64 word, unsigned thr, float scale, float (&v)[8]) {
+  u64 at = base + word * kGolden;
+#pragma unroll
+  for (int i = 0; i < 4; ++i, at += kGolden) {
+    const u64 w = splitmix(at);
+    v[2 * i] = (unsigned)w < thr ? 0.f : v[2 * i] * scale;
+    v[2 * i + 1] = (unsigned)(w >> 32) < thr ? 0.f : v[2 * i + 1] * scale;
+  }
+}
+
+// ---- activations.  a(z) and a'(z):
+//   ReLU        max(z, 0)                                 1 where z > 0
+//   GELU        z Phi(z)                                  Phi(z) + z phi(z)             (normal distribution and its density)
+//   GELU, tanh  z s,  s = 1/(1+exp(-2u)),                 s + z s (1 - s) 2 u',  u' = c (1 + 3*0.044715 z^2)
+//               u = c (z + 0.044715 z^3), c = sqrt(2/pi)  (z/2 (1 + tanh u) is the same function)
+//   SiLU        z s,  s = 1/(1+exp(-z))                   s + z s (1 - s)
+constexpr float kGeluC = 0.7978845608028654f, kGeluK = 0.044715f, kInvSqrt2 = 0.7071067811865476f, kInvSqrt2Pi = 0.3989422804014327f;
+__device__ inline float sigmoid_f(float x) { return 1.f / (1.f + expf(-x)); }
+template <int V> __device__ inline void activate(float (&v)[V], int act) {
+  if (act == RESIST_ACT_RELU) {
+#pragma unroll
+    for (int e = 0; e < V; ++e) v[e] = v[e] > 0.f ? v[e] : 0.f;
+  } else if (act == RESIST_ACT_GELU) {
+#pragma unroll
+    for (int e = 0; e < V; ++e) v[e] = v[e] * (0.5f * erfcf(-v[e] * kInvSqrt2));
+  } else if (act == RESIST_ACT_GELU_TANH) {
+#pragma unroll
+    for (int e = 0; e < V; ++e) v[e] = v[e] * sigmoid_f(2.f * kGeluC * (v[e] + kGeluK * v[e] * v[e] * v[e]));
+  } else if (act == RESIST_ACT_SILU) {
+#pragma unroll
+    for (int e = 0; e < V; ++e) v[e] = v[e] * sigmoid_f(v[e]);
+  }
+}
+// v[e] *= a'(z[e]).  Far out, where a' is 0 or 1 to the last bit, z is held back: its own growth would meet that zero as infinity.
+__device__ inline float held(float z, float most) { return z > most ? most : z < -most ? -most : z; }   // a NaN stays one
+template <int V> __device__ inline void times_slope(float (&v)[V], const float (&z)[V], int act) {
+  if (act == RESIST_ACT_RELU) {
+#pragma unroll
+    for (int e = 0; e < V; ++e) v[e] = z[e] > 0.f ? v[e] : 0.f;
+  } else if (act == RESIST_ACT_GELU) {
+#pragma unroll
+    for (int e = 0; e < V; ++e) {
+      const float t = held(z[e], 20.f);
+      v[e] *= 0.5f * erfcf(-t * kInvSqrt2) + t * kInvSqrt2Pi * expf(-0.5f * t * t);
+    }
+  } else if (act == RESIST_ACT_GELU_TANH) {
+#pragma unroll
+    for (int e = 0; e < V; ++e) {
+      const float t = held(z[e], 20.f), s = sigmoid_f(2.f * kGeluC * (t + kGeluK * t * t * t));
+      v[e] *= s + t * s * (1.f - s) * 2.f * kGeluC * (1.f + 3.f * kGeluK * t * t);
+    }
+  } else if (act == RESIST_ACT_SILU) {
+#pragma unroll
+    for (int e = 0; e < V; ++e) {
+      const float t = held(z[e], 200.f), s = sigmoid_f(t);
+      v[e] *= s + t * s * (1.f - s);
+    }
+  }
+}
+
+}  // namespace resist

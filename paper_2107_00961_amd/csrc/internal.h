@@ -252,4 +252,22 @@ struct AggSeg { float *dst; const float *src[16]; int count; int64_t n; };
 int aggregate_f32(const std::vector<AggSeg> &segs, hipStream_t st);
 int fill_zero_f32(float *p, int64_t n, hipStream_t st);
 
+// operators of a dense residual block (layernorm.hip, dropout.hip, linear.hip); row strides in elements, arguments checked by dense_ops.cpp
+struct LayerNorm { int64_t M; int N; const void *x; int64_t ldx; const float *gamma, *beta; float *mean, *rstd; float eps; };
+int layernorm_fwd(int dt, const LayerNorm &l, void *y, int64_t ldy, hipStream_t st);
+int64_t layernorm_workspace_floats(int64_t M, int N);
+int layernorm_bwd(int dt, const LayerNorm &l, const void *dy, int64_t lddy, const void *addend, int64_t lda, void *dx, int64_t lddx,
+                  float *dgamma, float *dbeta, float *work, hipStream_t st);
+struct DropSpec { double p; const uint64_t *rng; };   // rng: device {seed, offset}, NULL where p is 0
+// out = [res +] [a'(z) *] dropout(x); res and z not both
+int dropout(int dt, int64_t M, int N, const void *x, int64_t ldx, const void *res, int64_t ldr, int act, const void *z, int64_t ldz,
+            const DropSpec &d, void *out, int64_t ldo, hipStream_t st);
+struct LinearShape { int64_t M; int K, N; int64_t ldx, ldy; };
+struct LinearEpilogue { const float *bias; int act; DropSpec drop; const void *residual; int64_t ldr; void *z; int64_t ldz; };
+struct LinearThrough { int act; const void *z; int64_t ldz; DropSpec drop; };
+int64_t linear_workspace(const LinearShape &s, int dt, int op);   // bytes; op 0 forward, 1 data gradient, 2 weight gradient
+int linear_fwd(const LinearShape &s, int dt, const void *x, const void *w, const LinearEpilogue &e, void *y, void *work, hipStream_t st);
+int linear_dgrad(const LinearShape &s, int dt, const void *dz, const void *w, const LinearThrough &t, void *dx, void *work, hipStream_t st);
+int linear_wgrad(const LinearShape &s, int dt, const void *dz, const void *x, float *dw, float *db, void *work, hipStream_t st);
+
 }  // namespace resist
