@@ -93,6 +93,290 @@ __global__ __launch_bounds__(kThreads) void gemm_any_kernel(GemmArgs g) {
   }
 }
 
+// ---- bf16 operands, tiled -------------------------------------------------------------------------------------------
+// Operand tiles go from memory straight into LDS (16 bytes a lane, 1 KB a wave and instruction, in lane order), STAGES deep, and from there
+// in fragments to the matrix cores.  Four waves, a quarter of the BM x BN tile each: the larger a wave's share, the fewer times a
+// staged element is read from LDS (256x256: 1024 clocks of reading and 512 of arriving for 2048 of products).
+// Layout in LDS.  Lane order leaves no room for padding, so what keeps rows off each other's banks is which 16-byte piece a lane asks for:
+//   reduction contiguous (R): a row is an index i, BK values of r: piece c of row i lies at c ^ f(i), f = i & 7 (BK 64, 128 bytes a row),
+//     (i >> 1) & 3 (BK 32, two rows to 128 bytes): eight consecutive rows' pieces c fill 128 bytes;
+//   other index contiguous: a row is an r, BM values of i: piece c of row r lies at c ^ 4 (r & 3): the four rows of a transpose
+//     read, 64 bytes each, fill 256 bytes.
+// Bounds: an operand's descriptor starts at the tile and ends with the operand (rows past it, and steps past it, come as zeros); its
+// contiguous axis is a multiple of eight where it is the reduction (a tail's pieces are not asked for) and may end in a piece where it is
+// not (what a tile has past its last column goes into outputs that are not stored).
+template <bool R, int B, int BK> struct Stage {
+  static constexpr int kBytes = B * BK * 2, kLoads = kBytes / 4096;   // a wave's instructions
+  static constexpr int kRow = R ? BK * 2 : B * 2, kPieces = kRow / 16, kRows = 1024 / kRow;   // rows an instruction
+  // row and piece of the tile that lane `l` of wave `w` asks for with instruction p
+  __device__ static inline int row(int p, int w, int l) { return (p * 4 + w) * kRows + l / kPieces; }
+  __device__ static inline int piece(int r, int l) {
+    const int f = R ? (BK == 64 ? r & 7 : (r >> 1) & 3) : (r & 3) << 2;
+    return (l % kPieces) ^ f;
+  }
+};
+
+struct TileArgs {
+  const __bf16 *a, *b;
+  long long lda, ldb;       // elements between rows (of i, or of r)
+  long long I, R;
+  int J, tiles_i, tiles_j, group;
+  int splits;
+  long long per_split;      // steps of the reduction, a multiple of the tile's
+  float *part;              // [splits][I][J] where the reduction is split
+  Epilogue e;
+};
+
+// eight outputs of a row
+template <typename O>
+__device__ inline void finish8(const Epilogue &e, long long i, int j, int left, float (&v)[8], u64 base) {
+  if (e.bias) {
+    float b[8];
+    row_load(e.bias + j, left, b);
+#pragma unroll
+    for (int k = 0; k < 8; ++k) v[k] += b[k];
+  }
+  if (e.z_out) row_store(static_cast<O *>(e.z_out) + i * e.ldz + j, left, v);
+  if (!e.z_in) activate(v, e.act);
+  if (e.d.rng) dropout8(base, (u64)i * (unsigned)e.words + (unsigned)(j >> 1), e.d.thr, e.d.scale, v);
+  if (e.z_in) {
+    float z[8];
+    row_load(static_cast<const O *>(e.z_in) + i * e.ldz + j, left, z);
+    times_slope(v, z, e.act);
+  }
+  if (e.res) {
+    float r[8];
+    row_load(static_cast<const O *>(e.res) + i * e.ldr + j, left, r);
+#pragma unroll
+    for (int k = 0; k < 8; ++k) v[k] += r[k];
+  }
+  row_store(static_cast<O *>(e.out) + i * e.ldo + j, left, v);
+}
+
+template <int N> __device__ inline void wait_and_meet() {   // at most N of this wave's transfers to LDS under way, all of its reads done
+  asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(N) : "memory");
+}
+
+// of a scheduling region: MF products, DS LDS reads between the first half of them and VM transfers between the others (a transfer to LDS
+// stays behind the reads that stand before it)
+template <int M, int MF, int DS, int VM> __device__ inline void spread_one() {
+  if constexpr (M < MF) {
+    __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+    constexpr int H = MF / 2, lo = M < H ? M : H, hi = M < H ? M + 1 : H;
+    constexpr int ds = hi * DS / H - lo * DS / H, vm = M < H ? 0 : (M - H + 1) * VM / H - (M - H) * VM / H;
+    if constexpr (ds > 0) __builtin_amdgcn_sched_group_barrier(0x100, ds, 0);
+    if constexpr (vm > 0) __builtin_amdgcn_sched_group_barrier(0x010, vm, 0);
+    spread_one<M + 1, MF, DS, VM>();
+  }
+}
+
+// the tile's place: `group` rows of tiles are walked column by column, an XCD's workgroups one after the other
+__device__ inline void tile_of(int bid, int tiles_i, int tiles_j, int group, int &ti, int &tj) {
+  const int per = group * tiles_j, g = bid / per, rest = bid - g * per;
+  const int rows = min(group, tiles_i - g * group);
+  tj = rest / rows;
+  ti = g * group + rest - tj * rows;
+}
+
+template <typename O, bool AR, bool BR, int BM, int BN, int BK, int STAGES, int WGS>
+__global__ __launch_bounds__(kThreads, WGS) void gemm_tile_kernel(TileArgs g) {
+  using SA = Stage<AR, BM, BK>;
+  using SB = Stage<BR, BN, BK>;
+  constexpr int WTM = BM / 2, WTN = BN / 2, TM = WTM / 32, TN = WTN / 32, NK = BK / 16;
+  constexpr int kStage = SA::kBytes + SB::kBytes, kLoads = SA::kLoads + SB::kLoads;
+  constexpr int kPitch = WTN * 4 + 16, kOut = 4 * 32 * kPitch;
+  static_assert(STAGES >= 2 && (STAGES - 2) * kLoads < 64, "stages");
+  __shared__ __attribute__((aligned(1024))) char lds[STAGES * kStage > kOut ? STAGES * kStage : kOut];
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), wm = wave >> 1, wn = wave & 1;
+  int ti, tj, bid = xcd_contiguous(blockIdx.x, gridDim.x);
+  const int split = bid / (g.tiles_i * g.tiles_j);
+  tile_of(bid - split * g.tiles_i * g.tiles_j, g.tiles_i, g.tiles_j, g.group, ti, tj);
+  const long long i0 = (long long)ti * BM, rbeg = split * g.per_split, rend = min(g.R, rbeg + g.per_split);
+  const int j0 = tj * BN;
+  const int steps = (int)((rend - rbeg + BK - 1) / BK);
+
+  // ---- operands to LDS.  left: bytes from the tile's current corner to the operand's end
+  const char *pa = reinterpret_cast<const char *>(g.a + (AR ? i0 * g.lda + rbeg : rbeg * g.lda + i0));
+  const char *pb = reinterpret_cast<const char *>(g.b + (BR ? (long long)j0 * g.ldb + rbeg : rbeg * g.ldb + j0));
+  long long left_a = AR ? ((g.I - i0 - 1) * g.lda + (rend - rbeg)) * 2 : ((rend - rbeg - 1) * g.lda + (g.I - i0 + 7) / 8 * 8) * 2;
+  long long left_b = BR ? ((g.J - j0 - 1) * g.ldb + (rend - rbeg)) * 2 : ((rend - rbeg - 1) * g.ldb + (g.J - j0 + 7) / 8 * 8) * 2;
+  unsigned va[SA::kLoads], vb[SB::kLoads];
+#pragma unroll
+  for (int p = 0; p < SA::kLoads; ++p) {
+    const int r = SA::row(p, wave, lane);
+    va[p] = (unsigned)(r * g.lda * 2) + SA::piece(r, lane) * 16;
+  }
+#pragma unroll
+  for (int p = 0; p < SB::kLoads; ++p) {
+    const int r = SB::row(p, wave, lane);
+    vb[p] = (unsigned)(r * g.ldb * 2) + SB::piece(r, lane) * 16;
+  }
+  // of a row of BK reduction steps: the first step of this lane's piece (the same in every instruction)
+  const int ka = SA::piece(SA::row(0, wave, lane), lane) * 8, kb = SB::piece(SB::row(0, wave, lane), lane) * 8;
+  int left_r = (int)min(rend - rbeg, (long long)0x40000000);
+  auto request = [&](int first, int last, int stage) {   // instructions first .. last-1 of the step
+    const __amdgpu_buffer_rsrc_t ra = make_rsrc(pa, left_a > 0 ? (unsigned)min(left_a, 0x7ffffff0LL) : 0u);
+    const __amdgpu_buffer_rsrc_t rb = make_rsrc(pb, left_b > 0 ? (unsigned)min(left_b, 0x7ffffff0LL) : 0u);
+    char *to = lds + stage * kStage + wave * 1024;
+#pragma unroll
+    for (int p = 0; p < kLoads; ++p) {
+      if (p < first || p >= last) continue;
+      const bool is_a = p < SA::kLoads;
+      unsigned v = is_a ? va[p] : vb[p - SA::kLoads];
+      if (is_a ? AR : BR) v = (is_a ? ka : kb) < left_r ? v : kOOB;
+      char *dst = to + (is_a ? p * 4096 : SA::kBytes + (p - SA::kLoads) * 4096);
+      __builtin_amdgcn_raw_ptr_buffer_load_lds(is_a ? ra : rb, (__attribute__((address_space(3))) void *)dst, 16, (int)v, 0, 0, 0);
+    }
+  };
+  auto advance = [&]() {
+    const long long da = (AR ? BK : BK * g.lda) * 2, db = (BR ? BK : BK * g.ldb) * 2;
+    pa += da; left_a -= da;
+    pb += db; left_b -= db;
+    left_r -= BK;
+  };
+
+  // ---- fragments from LDS: eight consecutive steps of the reduction of one index per lane, as they lie or by two transpose reads
+  const int lr = lane & 31, lg = lane >> 5;
+  int oa[AR ? NK : TM], ob[BR ? NK : TN];
+  if constexpr (AR) {
+#pragma unroll
+    for (int k = 0; k < NK; ++k) oa[k] = (wm * WTM + lr) * SA::kRow + (((k * 2 + lg) ^ (BK == 64 ? lr & 7 : (lr >> 1) & 3)) << 4);
+  } else {
+    const int fr = lg * 8 + ((lane & 15) >> 2), fc = ((lane >> 4) & 1) * 16 + (lane & 3) * 4;
+#pragma unroll
+    for (int i = 0; i < TM; ++i) {
+      const int c = wm * WTM + i * 32 + fc;
+      oa[i] = fr * SA::kRow + (((c >> 3) ^ ((fr & 3) << 2)) << 4) + (c & 7) * 2;
+    }
+  }
+  if constexpr (BR) {
+#pragma unroll
+    for (int k = 0; k < NK; ++k) ob[k] = (wn * WTN + lr) * SB::kRow + (((k * 2 + lg) ^ (BK == 64 ? lr & 7 : (lr >> 1) & 3)) << 4);
+  } else {
+    const int fr = lg * 8 + ((lane & 15) >> 2), fc = ((lane >> 4) & 1) * 16 + (lane & 3) * 4;
+#pragma unroll
+    for (int j = 0; j < TN; ++j) {
+      const int c = wn * WTN + j * 32 + fc;
+      ob[j] = fr * SB::kRow + (((c >> 3) ^ ((fr & 3) << 2)) << 4) + (c & 7) * 2;
+    }
+  }
+  bf16x8 fa[2][TM], fb[2][TN];
+  auto fetch = [&](int set, int stage, int k) {
+    const char *A = lds + stage * kStage, *B = A + SA::kBytes;
+#pragma unroll
+    for (int i = 0; i < TM; ++i) {
+      if constexpr (AR) fa[set][i] = *reinterpret_cast<const bf16x8 *>(A + oa[k] + i * 32 * SA::kRow);
+      else fa[set][i] = lds_read_tr_pair(A + oa[i] + k * 16 * SA::kRow, A + oa[i] + (k * 16 + 4) * SA::kRow);
+    }
+#pragma unroll
+    for (int j = 0; j < TN; ++j) {
+      if constexpr (BR) fb[set][j] = *reinterpret_cast<const bf16x8 *>(B + ob[k] + j * 32 * SB::kRow);
+      else fb[set][j] = lds_read_tr_pair(B + ob[j] + k * 16 * SB::kRow, B + ob[j] + (k * 16 + 4) * SB::kRow);
+    }
+  };
+
+  f32x16 acc[TM][TN];
+#pragma unroll
+  for (int i = 0; i < TM; ++i)
+#pragma unroll
+    for (int j = 0; j < TN; ++j)
+#pragma unroll
+      for (int e = 0; e < 16; ++e) acc[i][j][e] = 0.f;
+
+#pragma unroll
+  for (int s = 0; s < STAGES - 1; ++s) {
+    request(0, kLoads, s);
+    advance();
+  }
+  wait_and_meet<(STAGES - 2) * kLoads>();
+  fetch(0, 0, 0);
+  __builtin_amdgcn_sched_barrier(0);
+  int stage = 0, refill = STAGES - 1;
+  auto step = [&](auto kc, int next) {
+    constexpr int k = decltype(kc)::value;
+    constexpr int v0 = k * kLoads / (NK - 1), v1 = k + 1 < NK ? (k + 1) * kLoads / (NK - 1) : v0;
+    if constexpr (k + 1 < NK) {
+      fetch((k + 1) & 1, stage, k + 1);
+      request(v0, v1, refill);
+    } else {
+      advance();
+      wait_and_meet<(STAGES - 2) * kLoads>();
+      fetch(0, next, 0);
+    }
+#pragma unroll
+    for (int i = 0; i < TM; ++i)
+#pragma unroll
+      for (int j = 0; j < TN; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fb[k & 1][j], fa[k & 1][i], acc[i][j], 0, 0, 0);
+    spread_one<0, TM * TN, (AR ? TM : 2 * TM) + (BR ? TN : 2 * TN), v1 - v0>();   // the next step's reads, and transfers, between this one's products
+    __builtin_amdgcn_sched_barrier(0);
+  };
+  for (int t = 0; t < steps; ++t) {
+    const int next = stage + 1 == STAGES ? 0 : stage + 1;
+    step(std::integral_constant<int, 0>{}, next);
+    step(std::integral_constant<int, 1>{}, next);
+    if constexpr (NK > 2) {
+      step(std::integral_constant<int, 2>{}, next);
+      step(std::integral_constant<int, 3>{}, next);
+    }
+    refill = stage;
+    stage = next;
+  }
+
+  // ---- out: 32 rows of a wave's share at a time through LDS, so that memory sees whole rows of it
+  asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");   // the steps past the end have arrived too
+  char *const mine = lds + wave * 32 * kPitch;
+  const u64 base = g.e.d.rng && g.splits == 1 ? dropout_base(g.e.d.rng) : 0;
+  constexpr int LPR = WTN / 8, RPP = 64 / LPR;   // lanes a row, rows a pass
+  const int c = (lane % LPR) * 8, j = j0 + wn * WTN + c, left = g.J - j;
+#pragma unroll 1
+  for (int i = 0; i < TM; ++i) {   // one copy of what follows: it is long, and the instruction cache is shared
+#pragma unroll
+    for (int k = 0; k < TM; ++k)
+      if (k == i) {
+#pragma unroll
+        for (int n = 0; n < TN; ++n)
+#pragma unroll
+          for (int q = 0; q < 4; ++q)
+            *reinterpret_cast<f32x4 *>(mine + lr * kPitch + (n * 32 + q * 8 + lg * 4) * 4) = f32x4{acc[k][n][q * 4], acc[k][n][q * 4 + 1], acc[k][n][q * 4 + 2], acc[k][n][q * 4 + 3]};
+      }
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+#pragma unroll 1
+    for (int p = 0; p < 32 / RPP; ++p) {
+      const int r = p * RPP + lane / LPR;
+      const long long row = i0 + wm * WTM + i * 32 + r;
+      if (row >= g.I || left <= 0) continue;
+      float v[8];
+      const f32x4 lo = *reinterpret_cast<const f32x4 *>(mine + r * kPitch + c * 4), hi = *reinterpret_cast<const f32x4 *>(mine + r * kPitch + c * 4 + 16);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) { v[e] = lo[e]; v[e + 4] = hi[e]; }
+      if (g.splits > 1) row_store(g.part + ((long long)split * g.I + row) * g.J + j, left, v);
+      else finish8<O>(g.e, row, j, left, v, base);
+    }
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+  }
+}
+
+// the parts of a split reduction, in order
+template <typename O>
+__global__ __launch_bounds__(kThreads) void gemm_join_kernel(const float *part, int splits, long long I, int J, Epilogue e) {
+  const int nvec = (J + 7) / 8;
+  const long long u = (long long)blockIdx.x * kThreads + threadIdx.x;
+  const long long row = u / nvec;
+  const int j = (int)(u - row * nvec) * 8, left = J - j;
+  if (row >= I) return;
+  float v[8];
+  row_load(part + row * J + j, left, v);
+  for (int s = 1; s < splits; ++s) {
+    float w[8];
+    row_load(part + ((long long)s * I + row) * J + j, left, w);
+#pragma unroll
+    for (int k = 0; k < 8; ++k) v[k] += w[k];
+  }
+  finish8<O>(e, row, j, left, v, e.d.rng ? dropout_base(e.d.rng) : 0);
+}
+
 // db: 64 columns of dz to a workgroup, four ranges of rows
 template <typename T>
 __global__ __launch_bounds__(kThreads) void col_sum_kernel(const T *dz, long long M, int N, long long ld, float *db) {
@@ -115,6 +399,18 @@ template <typename T, typename O, bool AR, bool BR> int gemm_any(GemmArgs &g, hi
   return RESIST_OK;
 }
 
+template <typename O, bool AR, bool BR> int gemm_tiles(TileArgs &t, hipStream_t st) {
+  t.tiles_i = (int)((t.I + 255) / 256);
+  t.tiles_j = (t.J + 255) / 256;
+  t.group = 8; t.splits = 1; t.per_split = (t.R + 63) / 64 * 64;
+#ifndef RESIST_CFG
+#define RESIST_CFG 256, 256, 32, 4, 1
+#endif
+  gemm_tile_kernel<O, AR, BR, RESIST_CFG><<<t.tiles_i * t.tiles_j, kThreads, 0, st>>>(t);
+  RESIST_CHECK_LAUNCH("linear");
+  return RESIST_OK;
+}
+
 }  // namespace
 
 int64_t linear_workspace(const LinearShape &s, int dt, int op) { (void)s; (void)dt; (void)op; return 0; }
@@ -126,6 +422,11 @@ int linear_fwd(const LinearShape &s, int dt, const void *x, const void *w, const
   g.b = w; g.bj = s.K; g.br = 1; g.J = s.N; g.R = s.K;
   g.e.out = y; g.e.ldo = s.ldy; g.e.bias = le.bias; g.e.z_out = le.z; g.e.ldz = le.ldz; g.e.res = le.residual; g.e.ldr = le.ldr;
   g.e.act = le.act; g.e.d = make_dropout(le.drop); g.e.words = (s.N + 1) / 2;
+  if (dt == DT_BF16 && s.K % 8 == 0 && s.ldx % 8 == 0) {
+    TileArgs t{};
+    t.a = (const __bf16 *)x; t.b = (const __bf16 *)w; t.lda = s.ldx; t.ldb = s.K; t.I = s.M; t.J = s.N; t.R = s.K; t.e = g.e;
+    return gemm_tiles<__bf16, true, true>(t, st);
+  }
   prof::Scope sc("linear_fwd", 2. * s.M * s.N * s.K, ((double)s.M * s.K + (double)s.N * s.K + (double)s.M * s.N) * esize(dt), st);
   return dt == DT_F32 ? gemm_any<float, float, true, true>(g, st) : gemm_any<__bf16, __bf16, true, true>(g, st);
 }
@@ -137,6 +438,11 @@ int linear_dgrad(const LinearShape &s, int dt, const void *dz, const void *w, co
   g.b = w; g.bj = 1; g.br = s.K; g.J = s.K; g.R = s.N;
   g.e.out = dx; g.e.ldo = s.ldx; g.e.z_in = lt.act == RESIST_ACT_NONE ? nullptr : lt.z; g.e.ldz = lt.ldz; g.e.act = lt.act;
   g.e.d = make_dropout(lt.drop); g.e.words = (s.K + 1) / 2;
+  if (dt == DT_BF16 && s.N % 8 == 0 && s.K % 8 == 0 && s.ldy % 8 == 0) {
+    TileArgs t{};
+    t.a = (const __bf16 *)dz; t.b = (const __bf16 *)w; t.lda = s.ldy; t.ldb = s.K; t.I = s.M; t.J = s.K; t.R = s.N; t.e = g.e;
+    return gemm_tiles<__bf16, true, false>(t, st);
+  }
   prof::Scope sc("linear_dgrad", 2. * s.M * s.N * s.K, ((double)s.M * s.K + (double)s.N * s.K + (double)s.M * s.N) * esize(dt), st);
   return dt == DT_F32 ? gemm_any<float, float, true, false>(g, st) : gemm_any<__bf16, __bf16, true, false>(g, st);
 }
@@ -146,7 +452,11 @@ int linear_wgrad(const LinearShape &s, int dt, const void *dz, const void *x, fl
   g.a = dz; g.ai = 1; g.ar = s.ldy; g.I = s.N;
   g.b = x; g.bj = 1; g.br = s.ldx; g.J = s.K; g.R = s.M;
   g.e.out = dw; g.e.ldo = s.K;
-  if (dw) {
+  if (dw && dt == DT_BF16 && s.ldx % 8 == 0 && s.ldy % 8 == 0) {
+    TileArgs t{};
+    t.a = (const __bf16 *)dz; t.b = (const __bf16 *)x; t.lda = s.ldy; t.ldb = s.ldx; t.I = s.N; t.J = s.K; t.R = s.M; t.e = g.e;
+    RESIST_TRY((gemm_tiles<float, false, false>(t, st)));
+  } else if (dw) {
     prof::Scope sc("linear_wgrad", 2. * s.M * s.N * s.K, ((double)s.M * s.K + (double)s.M * s.N) * esize(dt) + 4. * s.N * s.K, st);
     RESIST_TRY((dt == DT_F32 ? gemm_any<float, float, false, false>(g, st) : gemm_any<__bf16, float, false, false>(g, st)));
   }
