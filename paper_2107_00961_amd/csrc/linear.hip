@@ -127,47 +127,43 @@ struct TileArgs {
   Epilogue e;
 };
 
-// eight outputs of a row
+// eight outputs of a row.  bias: of their columns; side: what the epilogue reads beside them, z (data gradient) or the residual (forward)
 template <typename O>
-__device__ inline void finish8(const Epilogue &e, long long i, int j, int left, float (&v)[8], u64 base) {
-  if (e.bias) {
-    float b[8];
-    row_load(e.bias + j, left, b);
+__device__ inline void finish8(const Epilogue &e, long long i, int j, int left, float (&v)[8], const float (&bias)[8], const Raw8<O> &side, u64 base) {
 #pragma unroll
-    for (int k = 0; k < 8; ++k) v[k] += b[k];
-  }
+  for (int k = 0; k < 8; ++k) v[k] += bias[k];
   if (e.z_out) row_store(static_cast<O *>(e.z_out) + i * e.ldz + j, left, v);
   if (!e.z_in) activate(v, e.act);
   if (e.d.rng) dropout8(base, (u64)i * (unsigned)e.words + (unsigned)(j >> 1), e.d.thr, e.d.scale, v);
-  if (e.z_in) {
-    float z[8];
-    row_load(static_cast<const O *>(e.z_in) + i * e.ldz + j, left, z);
-    times_slope(v, z, e.act);
-  }
-  if (e.res) {
-    float r[8];
-    row_load(static_cast<const O *>(e.res) + i * e.ldr + j, left, r);
+  if (e.z_in || e.res) {
+    float s[8];
+    widen(side, s);
+    if (e.z_in) {
+      times_slope(v, s, e.act);
+    } else {
 #pragma unroll
-    for (int k = 0; k < 8; ++k) v[k] += r[k];
+      for (int k = 0; k < 8; ++k) v[k] += s[k];
+    }
   }
   row_store(static_cast<O *>(e.out) + i * e.ldo + j, left, v);
 }
-
-template <int N> __device__ inline void wait_and_meet() {   // at most N of this wave's transfers to LDS under way, all of its reads done
-  asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(N) : "memory");
+template <typename O> __device__ inline const O *side_of(const Epilogue &e, long long &ld) {
+  ld = e.z_in ? e.ldz : e.ldr;
+  return static_cast<const O *>(e.z_in ? e.z_in : e.res);
+}
+__device__ inline void bias_of(const Epilogue &e, int j, int left, float (&b)[8]) {
+#pragma unroll
+  for (int k = 0; k < 8; ++k) b[k] = 0.f;
+  if (e.bias) row_load(e.bias + j, left, b);
 }
 
-// of a scheduling region: MF products, DS LDS reads between the first half of them and VM transfers between the others (a transfer to LDS
-// stays behind the reads that stand before it)
-template <int M, int MF, int DS, int VM> __device__ inline void spread_one() {
-  if constexpr (M < MF) {
-    __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
-    constexpr int H = MF / 2, lo = M < H ? M : H, hi = M < H ? M + 1 : H;
-    constexpr int ds = hi * DS / H - lo * DS / H, vm = M < H ? 0 : (M - H + 1) * VM / H - (M - H) * VM / H;
-    if constexpr (ds > 0) __builtin_amdgcn_sched_group_barrier(0x100, ds, 0);
-    if constexpr (vm > 0) __builtin_amdgcn_sched_group_barrier(0x010, vm, 0);
-    spread_one<M + 1, MF, DS, VM>();
-  }
+// 16 bytes a lane from a buffer to LDS at `to` and on, in lane order.  Written out because the compiler, which sees that LDS is written, waits for
+// all transfers before the next read of any of it; what is waited for, and where, is wait_and_meet's.
+__device__ inline void transfer(__amdgpu_buffer_rsrc_t r, unsigned off, unsigned to) {
+  asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tbuffer_load_dwordx4 %0, %1, 0 offen lds" ::"v"(off), "s"(r), "s"(to) : "memory");
+}
+template <int N> __device__ inline void wait_and_meet() {   // at most N of this wave's transfers to LDS under way, all of its reads done
+  asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(N) : "memory");
 }
 
 // the tile's place: `group` rows of tiles are walked column by column, an XCD's workgroups one after the other
@@ -184,8 +180,9 @@ __global__ __launch_bounds__(kThreads, WGS) void gemm_tile_kernel(TileArgs g) {
   using SB = Stage<BR, BN, BK>;
   constexpr int WTM = BM / 2, WTN = BN / 2, TM = WTM / 32, TN = WTN / 32, NK = BK / 16;
   constexpr int kStage = SA::kBytes + SB::kBytes, kLoads = SA::kLoads + SB::kLoads;
-  constexpr int kPitch = WTN * 4 + 16, kOut = 4 * 32 * kPitch;
-  static_assert(STAGES >= 2 && (STAGES - 2) * kLoads < 64, "stages");
+  constexpr int kPitch = WTN * 4 + 16, kOut = 4 * 2 * 32 * kPitch;
+  static_assert(STAGES >= 2, "stages");
+  static_assert(TM <= 4, "tile");
   __shared__ __attribute__((aligned(1024))) char lds[STAGES * kStage > kOut ? STAGES * kStage : kOut];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), wm = wave >> 1, wn = wave & 1;
   int ti, tj, bid = xcd_contiguous(blockIdx.x, gridDim.x);
@@ -214,19 +211,14 @@ __global__ __launch_bounds__(kThreads, WGS) void gemm_tile_kernel(TileArgs g) {
   // of a row of BK reduction steps: the first step of this lane's piece (the same in every instruction)
   const int ka = SA::piece(SA::row(0, wave, lane), lane) * 8, kb = SB::piece(SB::row(0, wave, lane), lane) * 8;
   int left_r = (int)min(rend - rbeg, (long long)0x40000000);
-  auto request = [&](int first, int last, int stage) {   // instructions first .. last-1 of the step
-    const __amdgpu_buffer_rsrc_t ra = make_rsrc(pa, left_a > 0 ? (unsigned)min(left_a, 0x7ffffff0LL) : 0u);
-    const __amdgpu_buffer_rsrc_t rb = make_rsrc(pb, left_b > 0 ? (unsigned)min(left_b, 0x7ffffff0LL) : 0u);
-    char *to = lds + stage * kStage + wave * 1024;
-#pragma unroll
-    for (int p = 0; p < kLoads; ++p) {
-      if (p < first || p >= last) continue;
-      const bool is_a = p < SA::kLoads;
-      unsigned v = is_a ? va[p] : vb[p - SA::kLoads];
-      if (is_a ? AR : BR) v = (is_a ? ka : kb) < left_r ? v : kOOB;
-      char *dst = to + (is_a ? p * 4096 : SA::kBytes + (p - SA::kLoads) * 4096);
-      __builtin_amdgcn_raw_ptr_buffer_load_lds(is_a ? ra : rb, (__attribute__((address_space(3))) void *)dst, 16, (int)v, 0, 0, 0);
-    }
+  const unsigned lds_at = __builtin_amdgcn_readfirstlane((unsigned)(uintptr_t)(__attribute__((address_space(3))) char *)lds) + wave * 1024;
+  auto request = [&](int p, int stage) {   // instruction p of the step
+    const bool is_a = p < SA::kLoads;
+    const __amdgpu_buffer_rsrc_t r = is_a ? make_rsrc(pa, left_a > 0 ? (unsigned)min(left_a, 0x7ffffff0LL) : 0u)
+                                          : make_rsrc(pb, left_b > 0 ? (unsigned)min(left_b, 0x7ffffff0LL) : 0u);
+    unsigned v = is_a ? va[p] : vb[p - SA::kLoads];
+    if (is_a ? AR : BR) v = (is_a ? ka : kb) < left_r ? v : kOOB;
+    transfer(r, v, lds_at + stage * kStage + (is_a ? p * 4096 : SA::kBytes + (p - SA::kLoads) * 4096));
   };
   auto advance = [&]() {
     const long long da = (AR ? BK : BK * g.lda) * 2, db = (BR ? BK : BK * g.ldb) * 2;
@@ -261,15 +253,14 @@ __global__ __launch_bounds__(kThreads, WGS) void gemm_tile_kernel(TileArgs g) {
     }
   }
   bf16x8 fa[2][TM], fb[2][TN];
-  auto fetch = [&](int set, int stage, int k) {
+  auto fetch = [&](int n, int set, int stage, int k) {   // fragment n, in the order the products want them: A's first, B's, the rest of A's
     const char *A = lds + stage * kStage, *B = A + SA::kBytes;
-#pragma unroll
-    for (int i = 0; i < TM; ++i) {
+    if (n == 0 || n > TN) {
+      const int i = n == 0 ? 0 : n - TN;
       if constexpr (AR) fa[set][i] = *reinterpret_cast<const bf16x8 *>(A + oa[k] + i * 32 * SA::kRow);
       else fa[set][i] = lds_read_tr_pair(A + oa[i] + k * 16 * SA::kRow, A + oa[i] + (k * 16 + 4) * SA::kRow);
-    }
-#pragma unroll
-    for (int j = 0; j < TN; ++j) {
+    } else {
+      const int j = n - 1;
       if constexpr (BR) fb[set][j] = *reinterpret_cast<const bf16x8 *>(B + ob[k] + j * 32 * SB::kRow);
       else fb[set][j] = lds_read_tr_pair(B + ob[j] + k * 16 * SB::kRow, B + ob[j] + (k * 16 + 4) * SB::kRow);
     }
@@ -283,32 +274,41 @@ __global__ __launch_bounds__(kThreads, WGS) void gemm_tile_kernel(TileArgs g) {
 #pragma unroll
       for (int e = 0; e < 16; ++e) acc[i][j][e] = 0.f;
 
+  // A step of the reduction asks for the tile STAGES steps ahead, whose place in LDS is free once all waves have met at the end of
+  // the step before it: an NK-th of its transfers then, an NK-th with each of the first NK-1 of its NK products of depth 16.
+  constexpr int kEach = kLoads / NK;
+  static_assert(kLoads % NK == 0 && (STAGES - 2) * kLoads + kEach < 64, "transfers");
 #pragma unroll
   for (int s = 0; s < STAGES - 1; ++s) {
-    request(0, kLoads, s);
+#pragma unroll
+    for (int p = 0; p < kLoads; ++p) request(p, s);
     advance();
   }
-  wait_and_meet<(STAGES - 2) * kLoads>();
-  fetch(0, 0, 0);
+#pragma unroll
+  for (int p = 0; p < kEach; ++p) request(p, STAGES - 1);
+  wait_and_meet<(STAGES - 2) * kLoads + kEach>();
+#pragma unroll
+  for (int n = 0; n < TM + TN; ++n) fetch(n, 0, 0, 0);
   __builtin_amdgcn_sched_barrier(0);
   int stage = 0, refill = STAGES - 1;
   auto step = [&](auto kc, int next) {
-    constexpr int k = decltype(kc)::value;
-    constexpr int v0 = k * kLoads / (NK - 1), v1 = k + 1 < NK ? (k + 1) * kLoads / (NK - 1) : v0;
-    if constexpr (k + 1 < NK) {
-      fetch((k + 1) & 1, stage, k + 1);
-      request(v0, v1, refill);
-    } else {
+    constexpr int k = decltype(kc)::value, MF = TM * TN, DS = TM + TN, MD = MF * 3 / 4;
+    constexpr bool last = k + 1 == NK;
+    if constexpr (last) {
       advance();
       wait_and_meet<(STAGES - 2) * kLoads>();
-      fetch(0, next, 0);
     }
+    int ds = 0, vm = 0;
 #pragma unroll
-    for (int i = 0; i < TM; ++i)
+    for (int m = 0; m < MF; ++m) {   // a product, then what goes on beside it, in this order
+      const int i = m / TN, j = m % TN;
+      acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fb[k & 1][j], fa[k & 1][i], acc[i][j], 0, 0, 0);
 #pragma unroll
-      for (int j = 0; j < TN; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fb[k & 1][j], fa[k & 1][i], acc[i][j], 0, 0, 0);
-    spread_one<0, TM * TN, (AR ? TM : 2 * TM) + (BR ? TN : 2 * TN), v1 - v0>();   // the next step's reads, and transfers, between this one's products
-    __builtin_amdgcn_sched_barrier(0);
+      for (; ds < (m < MD ? (m + 1) * DS / MD : DS); ++ds) fetch(ds, (k + 1) & 1, last ? next : stage, last ? 0 : k + 1);
+#pragma unroll
+      for (; vm < (m < MF / 2 ? (m + 1) * kEach / (MF / 2) : kEach); ++vm) request(last ? vm : (k + 1) * kEach + vm, last ? stage : refill);
+      __builtin_amdgcn_sched_barrier(0);
+    }
   };
   for (int t = 0; t < steps; ++t) {
     const int next = stage + 1 == STAGES ? 0 : stage + 1;
@@ -322,39 +322,67 @@ __global__ __launch_bounds__(kThreads, WGS) void gemm_tile_kernel(TileArgs g) {
     stage = next;
   }
 
-  // ---- out: 32 rows of a wave's share at a time through LDS, so that memory sees whole rows of it
+  // ---- out: 32 rows of a wave's share at a time through LDS, so that memory sees whole rows of it.  One wave a SIMD has nothing to hide a
+  // wait behind but its own next rows: they are on their way from LDS, what the epilogue reads beside them for the next kAhead passes from
+  // memory, while a pass is worked on.  One copy of the code (it is long, and the instruction cache is shared).
   asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");   // the steps past the end have arrived too
-  char *const mine = lds + wave * 32 * kPitch;
-  const u64 base = g.e.d.rng && g.splits == 1 ? dropout_base(g.e.d.rng) : 0;
-  constexpr int LPR = WTN / 8, RPP = 64 / LPR;   // lanes a row, rows a pass
+  char *const mine = lds + wave * 2 * 32 * kPitch;
+  const bool whole = g.splits == 1;
+  const u64 base = g.e.d.rng && whole ? dropout_base(g.e.d.rng) : 0;
+  constexpr int LPR = WTN / 8, RPP = 64 / LPR, PASSES = 32 / RPP, kAhead = sizeof(O) == 2 ? 8 : 4;   // lanes a row, rows a pass, passes of 32 rows
   const int c = (lane % LPR) * 8, j = j0 + wn * WTN + c, left = g.J - j;
-#pragma unroll 1
-  for (int i = 0; i < TM; ++i) {   // one copy of what follows: it is long, and the instruction cache is shared
+  const long long row0 = i0 + wm * WTM + lane / LPR;
+  auto put = [&](auto kc) {
+    constexpr int k = decltype(kc)::value;
 #pragma unroll
-    for (int k = 0; k < TM; ++k)
-      if (k == i) {
+    for (int n = 0; n < TN; ++n)
 #pragma unroll
-        for (int n = 0; n < TN; ++n)
-#pragma unroll
-          for (int q = 0; q < 4; ++q)
-            *reinterpret_cast<f32x4 *>(mine + lr * kPitch + (n * 32 + q * 8 + lg * 4) * 4) = f32x4{acc[k][n][q * 4], acc[k][n][q * 4 + 1], acc[k][n][q * 4 + 2], acc[k][n][q * 4 + 3]};
-      }
+      for (int q = 0; q < 4; ++q)
+        *reinterpret_cast<f32x4 *>(mine + (k & 1) * 32 * kPitch + lr * kPitch + (n * 32 + q * 8 + lg * 4) * 4) =
+            f32x4{acc[k][n][q * 4], acc[k][n][q * 4 + 1], acc[k][n][q * 4 + 2], acc[k][n][q * 4 + 3]};
+    asm volatile("" ::"n"(k));   // left alone, the compiler makes one of the calls, with an index, and keeps the sums in memory for it
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
     __builtin_amdgcn_wave_barrier();
-#pragma unroll 1
-    for (int p = 0; p < 32 / RPP; ++p) {
-      const int r = p * RPP + lane / LPR;
-      const long long row = i0 + wm * WTM + i * 32 + r;
-      if (row >= g.I || left <= 0) continue;
-      float v[8];
-      const f32x4 lo = *reinterpret_cast<const f32x4 *>(mine + r * kPitch + c * 4), hi = *reinterpret_cast<const f32x4 *>(mine + r * kPitch + c * 4 + 16);
+  };
+  f32x4 v0, v1;
+  auto get = [&](int pass) {   // rows of pass `pass` of all
+    const char *p = mine + (pass / PASSES & 1) * 32 * kPitch + (pass % PASSES * RPP + lane / LPR) * kPitch + c * 4;
+    v0 = *reinterpret_cast<const f32x4 *>(p);
+    v1 = *reinterpret_cast<const f32x4 *>(p + 16);
+  };
+  long long ld_side;
+  const O *side = side_of<O>(g.e, ld_side);
+  const bool has_side = side != nullptr && whole;
+  Raw8<O> ahead[kAhead] = {};
+  auto ask = [&](int pass, Raw8<O> &r) {
+    const long long row = row0 + pass * RPP;
+    if (pass < TM * PASSES && row < g.I && left > 0) raw_load(side + row * ld_side + j, left, r);
+  };
+  float bias[8] = {};
+  if (whole) bias_of(g.e, j, left, bias);
+  if (has_side) {
 #pragma unroll
-      for (int e = 0; e < 4; ++e) { v[e] = lo[e]; v[e + 4] = hi[e]; }
-      if (g.splits > 1) row_store(g.part + ((long long)split * g.I + row) * g.J + j, left, v);
-      else finish8<O>(g.e, row, j, left, v, base);
+    for (int p = 0; p < kAhead; ++p) ask(p, ahead[p]);
+  }
+  put(std::integral_constant<int, 0>{});
+  get(0);
+#pragma unroll 1
+  for (int pass = 0; pass < TM * PASSES; ++pass) {
+    if (TM > 1 && pass == 0) put(std::integral_constant<int, TM - 1 < 1 ? TM - 1 : 1>{});
+    if (TM > 2 && pass == PASSES) put(std::integral_constant<int, TM - 1 < 2 ? TM - 1 : 2>{});
+    if (TM > 3 && pass == 2 * PASSES) put(std::integral_constant<int, TM - 1 < 3 ? TM - 1 : 3>{});
+    float v[8] = {v0[0], v0[1], v0[2], v0[3], v1[0], v1[1], v1[2], v1[3]};
+    get(pass + 1 < TM * PASSES ? pass + 1 : pass);
+    const Raw8<O> now = ahead[0];
+    if (has_side) {
+#pragma unroll
+      for (int p = 0; p + 1 < kAhead; ++p) ahead[p] = ahead[p + 1];
+      ask(pass + kAhead, ahead[kAhead - 1]);
     }
-    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-    __builtin_amdgcn_wave_barrier();
+    const long long row = row0 + pass * RPP;
+    if (row >= g.I || left <= 0) continue;
+    if (whole) finish8<O>(g.e, row, j, left, v, bias, now, base);
+    else row_store(g.part + ((long long)split * g.I + row) * g.J + j, left, v);
   }
 }
 
@@ -374,7 +402,13 @@ __global__ __launch_bounds__(kThreads) void gemm_join_kernel(const float *part, 
 #pragma unroll
     for (int k = 0; k < 8; ++k) v[k] += w[k];
   }
-  finish8<O>(e, row, j, left, v, e.d.rng ? dropout_base(e.d.rng) : 0);
+  float bias[8];
+  bias_of(e, j, left, bias);
+  long long ld;
+  const O *side = side_of<O>(e, ld);
+  Raw8<O> now = {};
+  if (side) raw_load(side + row * ld + j, left, now);
+  finish8<O>(e, row, j, left, v, bias, now, e.d.rng ? dropout_base(e.d.rng) : 0);
 }
 
 // db: 64 columns of dz to a workgroup, four ranges of rows
@@ -399,16 +433,19 @@ template <typename T, typename O, bool AR, bool BR> int gemm_any(GemmArgs &g, hi
   return RESIST_OK;
 }
 
-template <typename O, bool AR, bool BR> int gemm_tiles(TileArgs &t, hipStream_t st) {
-  t.tiles_i = (int)((t.I + 255) / 256);
-  t.tiles_j = (t.J + 255) / 256;
-  t.group = 8; t.splits = 1; t.per_split = (t.R + 63) / 64 * 64;
-#ifndef RESIST_CFG
-#define RESIST_CFG 256, 256, 32, 4, 1
-#endif
-  gemm_tile_kernel<O, AR, BR, RESIST_CFG><<<t.tiles_i * t.tiles_j, kThreads, 0, st>>>(t);
+template <typename O, bool AR, bool BR, int BM, int BN, int BK, int STAGES, int WGS> int gemm_tiles_of(TileArgs &t, hipStream_t st) {
+  t.tiles_i = (int)((t.I + BM - 1) / BM);
+  t.tiles_j = (int)((t.J + BN - 1) / BN);
+  t.group = 8; t.splits = 1; t.per_split = (t.R + BK - 1) / BK * BK;
+  gemm_tile_kernel<O, AR, BR, BM, BN, BK, STAGES, WGS><<<t.tiles_i * t.tiles_j, kThreads, 0, st>>>(t);
   RESIST_CHECK_LAUNCH("linear");
   return RESIST_OK;
+}
+#ifndef RESIST_CFG
+#define RESIST_CFG 256, 256, 64, 2, 1
+#endif
+template <typename O, bool AR, bool BR> int gemm_tiles(TileArgs &t, hipStream_t st) {
+  return gemm_tiles_of<O, AR, BR, RESIST_CFG>(t, st);
 }
 
 }  // namespace
