@@ -1,5 +1,6 @@
 """ctypes binding of libresist.so -- argument marshalling only (same names as include/resist.h)."""
 import ctypes as C
+import functools
 import os
 
 import numpy as np
@@ -476,44 +477,60 @@ def stem_conv2d_wgrad(dy, x, w_shape, stride, pad, stream=None):
 
 # ---- operators of a dense residual block ---------------------------------------------------------------------------
 # Matrices are two-dimensional tensors [rows, N].  Their rows may be apart (a slice of a wider matrix); one whose rows are not
-# contiguous or not 16-byte aligned at the start is copied first.  Results are new tensors on the stream the call runs on (the
-# current one, or `stream`).
+# contiguous or not 16-byte aligned at the start is copied first.  Results are new tensors, allocated for the stream the call runs on:
+# the current one, or `stream`.
 ACTIVATIONS = {"none": 0, "relu": 1, "gelu": 2, "gelu_tanh": 3, "silu": 4}
+_DTYPES = {}   # torch dtype -> code, filled by the first call (torch is imported where it is needed)
+_here = None
 
 
-class _On:
-    """The device of the call's tensors as the current device, and its stream (hipStream_t in .ptr); results and workspaces are
-    allocated for that stream."""
+def _make_here():
+    """_here(t, stream): the current stream (hipStream_t) where the call can run as things stand, on t's device; None where it has to be
+    moved there first (_there).  Most of these calls take less time than torch.cuda.current_stream() alone."""
+    import torch
+    _DTYPES.update({torch.float32: 0, torch.bfloat16: 1})
+    device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
+    raw = getattr(torch._C, "_cuda_getCurrentRawStream", lambda i: torch.cuda.current_stream(i).cuda_stream)
 
-    def __init__(self, tensor, stream):
-        import torch
-        if not tensor.is_cuda:
+    def here(t, stream):
+        if not t.is_cuda:
             raise ResistError("device tensors only: there is no CPU path")
-        if stream is not None and stream.device != tensor.device:
-            raise ResistError(f"a stream of {stream.device} for tensors on {tensor.device}")
-        self._guards = []
-        if tensor.device.index != torch.cuda.current_device():
-            self._guards.append(torch.cuda.device(tensor.device))
+        i = t.get_device()
         if stream is not None:
-            self._guards.append(torch.cuda.stream(stream))
-        self._torch, self._stream, self.device = torch, stream, tensor.device
+            if stream.device_index != i:
+                raise ResistError(f"a stream of device {stream.device_index} for tensors on {t.device}")
+            return None
+        return raw(i) if device() == i else None
+    return here
 
-    def __enter__(self):
-        for g in self._guards:
-            g.__enter__()
-        self.ptr = (self._stream or self._torch.cuda.current_stream()).cuda_stream
-        return self
 
-    def __exit__(self, *exc):
-        for g in reversed(self._guards):
-            g.__exit__(*exc)
+def _on(t, stream):
+    global _here
+    if _here is None:
+        _here = _make_here()
+    return _here(t, stream)
 
-    def uses(self, *tensors):
-        """The call's inputs: memory of theirs that is given back meanwhile waits for a stream that is not their own."""
-        if self._stream is not None:
-            for t in tensors:
-                if t is not None:
-                    t.record_stream(self._stream)
+
+def _there(call, stream, *args):
+    """The call with its first tensor's device as the current one, on `stream` (None: that device's current stream).  Memory of its inputs that is
+    given back meanwhile waits for a stream that is not their own."""
+    import torch
+    with torch.cuda.device(args[0].device):
+        if stream is None:
+            return call(*args)
+        with torch.cuda.stream(stream):
+            out = call(*args)
+            for t in args:
+                if torch.is_tensor(t) and t.is_cuda:
+                    t.record_stream(stream)
+            return out
+
+
+def _dtype_of(t):
+    code = _DTYPES.get(t.dtype)
+    if code is None:
+        raise ResistError(f"unsupported tensor dtype {t.dtype}")
+    return code
 
 
 def _matrix(t, what, like=None, shape=None):
@@ -522,47 +539,50 @@ def _matrix(t, what, like=None, shape=None):
         raise ResistError(f"{what}: a matrix [rows, N] is needed, got {tuple(t.shape)}")
     if like is not None and (t.dtype != like.dtype or t.device != like.device):
         raise ResistError(f"{what}: {t.dtype} on {t.device} beside {like.dtype} on {like.device}")
-    if shape is not None and tuple(t.shape) != tuple(shape):
-        raise ResistError(f"{what}: shape {tuple(t.shape)} where {tuple(shape)} is needed")
-    if t.shape[1] == 0:
+    m, n = t.shape
+    if shape is not None and (m, n) != shape:
+        raise ResistError(f"{what}: shape {(m, n)} where {shape} is needed")
+    if n == 0:
         raise ResistError(f"{what}: rows without elements")
-    if t.stride(1) != 1 and t.shape[1] > 1 or t.stride(0) < t.shape[1] and t.shape[0] > 1 or t.data_ptr() % 16:
+    if t.is_contiguous():
+        return t if t.data_ptr() % 16 == 0 else t.clone()
+    if t.stride(1) != 1 and n > 1 or t.stride(0) < n and m > 1 or t.data_ptr() % 16:
         import torch
         t = t.clone(memory_format=torch.contiguous_format)
     return t
 
 
 def _ld(t):
-    """Row stride for the library: 0 (dense) where there is no second row to say it."""
-    return t.stride(0) if t.shape[0] > 1 else 0
+    """Row stride for the library: 0 (dense) where there is no second row to say it, or no tensor."""
+    return t.stride(0) if t is not None and t.shape[0] > 1 else 0
 
 
 def _vector(t, what, n, like):
     """A parameter vector [n] float32, or None -> itself, contiguous and aligned."""
-    import torch
     if t is None:
         return None
-    if t.dtype != torch.float32 or t.device != like.device or tuple(t.shape) != (n,):
+    if _DTYPES.get(t.dtype) != 0 or t.device != like.device or t.dim() != 1 or t.shape[0] != n:
         raise ResistError(f"{what}: float32 [{n}] on {like.device} is needed, got {t.dtype} {tuple(t.shape)} on {t.device}")
-    return t if t.is_contiguous() and t.data_ptr() % 16 == 0 else t.clone(memory_format=torch.contiguous_format)
+    return t if t.is_contiguous() and t.data_ptr() % 16 == 0 else t.clone()
 
 
 def _rng_ptr(rng, p, like):
     """{seed, offset}: a device tensor of two 64-bit integers, read when the kernel runs."""
-    import torch
     if rng is None:
         if p:
             raise ResistError("rng: needed where p is not 0")
         return None
+    import torch
     if rng.dtype not in (torch.int64, torch.uint64) or rng.device != like.device or tuple(rng.shape) != (2,) or not rng.is_contiguous():
         raise ResistError(f"rng: two contiguous 64-bit integers on {like.device} are needed")
     return rng.data_ptr()
 
 
 def _activation(act):
-    if act not in ACTIVATIONS:
+    code = ACTIVATIONS.get(act)
+    if code is None:
         raise ResistError(f"act {act!r}: one of {', '.join(ACTIVATIONS)}")
-    return ACTIVATIONS[act]
+    return code
 
 
 def _opt(t):
@@ -571,86 +591,98 @@ def _opt(t):
 
 def layernorm_forward(x, gamma=None, beta=None, eps=1e-5, stream=None):
     """x [M, N] float32 or bfloat16; gamma, beta [N] float32 or None -> (y, mean [M], rstd [M])."""
+    st = _on(x, stream)
+    if st is None:
+        return _there(layernorm_forward, stream, x, gamma, beta, eps)
     import torch
-    with _On(x, stream) as on:
-        dt = _dtype_code(x)
-        x = _matrix(x, "x")
-        M, N = x.shape
-        gamma, beta = _vector(gamma, "gamma", N, x), _vector(beta, "beta", N, x)
-        on.uses(x, gamma, beta)
-        y = torch.empty((M, N), dtype=x.dtype, device=on.device)
-        mean = torch.empty(M, dtype=torch.float32, device=on.device)
-        rstd = torch.empty(M, dtype=torch.float32, device=on.device)
-        _check(lib().resist_layernorm_forward(M, N, dt, x.data_ptr(), _ld(x), _opt(gamma), _opt(beta), eps, y.data_ptr(), 0,
-                                              mean.data_ptr(), rstd.data_ptr(), on.ptr))
+    dt = _dtype_of(x)
+    x = _matrix(x, "x")
+    M, N = x.shape
+    gamma, beta = _vector(gamma, "gamma", N, x), _vector(beta, "beta", N, x)
+    y = x.new_empty((M, N))
+    mean, rstd = x.new_empty(M, dtype=torch.float32), x.new_empty(M, dtype=torch.float32)
+    _check(lib().resist_layernorm_forward(M, N, dt, x.data_ptr(), _ld(x), _opt(gamma), _opt(beta), eps, y.data_ptr(), 0, mean.data_ptr(),
+                                          rstd.data_ptr(), st))
     return y, mean, rstd
+
+
+@functools.lru_cache(maxsize=4096)
+def _layernorm_ws(M, N):
+    n = C.c_int64()
+    _check(lib().resist_layernorm_workspace_bytes(M, N, C.byref(n)))
+    return n.value
 
 
 def layernorm_backward(dy, x, gamma, mean, rstd, addend=None, stream=None):
     """Gradients of layernorm_forward: dy, x [M, N], gamma [N] or None, mean and rstd as it returned them; addend [M, N] or None is
     added to dx -> (dx, dgamma [N], dbeta [N])."""
+    st = _on(dy, stream)
+    if st is None:
+        return _there(layernorm_backward, stream, dy, x, gamma, mean, rstd, addend)
     import torch
-    with _On(x, stream) as on:
-        dt = _dtype_code(x)
-        x = _matrix(x, "x")
-        M, N = x.shape
-        dy = _matrix(dy, "dy", x, (M, N))
-        addend = _matrix(addend, "addend", x, (M, N)) if addend is not None else None
-        gamma = _vector(gamma, "gamma", N, x)
-        if mean is None or rstd is None:
-            raise ResistError("mean and rstd: those of layernorm_forward are needed")
-        mean, rstd = _vector(mean, "mean", M, x), _vector(rstd, "rstd", M, x)
-        on.uses(dy, x, gamma, mean, rstd, addend)
-        dx = torch.empty((M, N), dtype=x.dtype, device=on.device)
-        dparams = torch.empty((2, (N + 3) // 4 * 4), dtype=torch.float32, device=on.device)
-        n = C.c_int64()
-        _check(lib().resist_layernorm_workspace_bytes(M, N, C.byref(n)))
-        ws = torch.empty(n.value, dtype=torch.uint8, device=on.device)
-        dgamma, dbeta = dparams[0, :N], dparams[1, :N]
-        _check(lib().resist_layernorm_backward(M, N, dt, dy.data_ptr(), _ld(dy), x.data_ptr(), _ld(x), _opt(gamma), mean.data_ptr(),
-                                               rstd.data_ptr(), _opt(addend), _ld(addend) if addend is not None else 0, dx.data_ptr(), 0,
-                                               dgamma.data_ptr(), dbeta.data_ptr(), ws.data_ptr(), n.value, on.ptr))
+    dt = _dtype_of(dy)
+    dy = _matrix(dy, "dy")
+    M, N = dy.shape
+    x = _matrix(x, "x", dy, (M, N))
+    addend = _matrix(addend, "addend", dy, (M, N)) if addend is not None else None
+    gamma = _vector(gamma, "gamma", N, dy)
+    if mean is None or rstd is None:
+        raise ResistError("mean and rstd: those of layernorm_forward are needed")
+    mean, rstd = _vector(mean, "mean", M, dy), _vector(rstd, "rstd", M, dy)
+    dx = dy.new_empty((M, N))
+    dgamma, dbeta = dy.new_empty(N, dtype=torch.float32), dy.new_empty(N, dtype=torch.float32)
+    n = _layernorm_ws(M, N)
+    ws = dy.new_empty(n, dtype=torch.uint8)
+    _check(lib().resist_layernorm_backward(M, N, dt, dy.data_ptr(), _ld(dy), x.data_ptr(), _ld(x), _opt(gamma), mean.data_ptr(), rstd.data_ptr(),
+                                           _opt(addend), _ld(addend), dx.data_ptr(), 0, dgamma.data_ptr(), dbeta.data_ptr(), ws.data_ptr(), n, st))
     return dx, dgamma, dbeta
 
 
 def dropout_forward(x, p, rng, residual=None, stream=None):
     """[residual +] dropout(x), x [M, N]: elements dropped with probability p, the others times 1/(1-p).  rng: device tensor of two 64-bit
     integers {seed, offset}; a call uses M * ceil(N/2) numbers from `offset` on, the same rng, p and shape give the same mask."""
-    import torch
-    with _On(x, stream) as on:
-        dt = _dtype_code(x)
-        x = _matrix(x, "x")
-        M, N = x.shape
-        residual = _matrix(residual, "residual", x, (M, N)) if residual is not None else None
-        on.uses(x, rng, residual)
-        y = torch.empty((M, N), dtype=x.dtype, device=on.device)
-        _check(lib().resist_dropout_forward(M, N, dt, x.data_ptr(), _ld(x), p, _rng_ptr(rng, p, x), _opt(residual),
-                                            _ld(residual) if residual is not None else 0, y.data_ptr(), 0, on.ptr))
+    st = _on(x, stream)
+    if st is None:
+        return _there(dropout_forward, stream, x, p, rng, residual)
+    dt = _dtype_of(x)
+    x = _matrix(x, "x")
+    M, N = x.shape
+    residual = _matrix(residual, "residual", x, (M, N)) if residual is not None else None
+    y = x.new_empty((M, N))
+    _check(lib().resist_dropout_forward(M, N, dt, x.data_ptr(), _ld(x), p, _rng_ptr(rng, p, x), _opt(residual), _ld(residual), y.data_ptr(), 0, st))
     return y
 
 
 def dropout_backward(dy, p, rng, act="none", z=None, stream=None):
     """Gradient of dropout(act(z)) with respect to z [M, N] from dy [M, N] (act "none": of dropout alone, z is not read)."""
-    import torch
-    with _On(dy, stream) as on:
-        dt, code = _dtype_code(dy), _activation(act)
-        dy = _matrix(dy, "dy")
-        M, N = dy.shape
-        if code and z is None:
-            raise ResistError("z: needed for the gradient of an activation")
-        z = _matrix(z, "z", dy, (M, N)) if code else None
-        on.uses(dy, rng, z)
-        dx = torch.empty((M, N), dtype=dy.dtype, device=on.device)
-        _check(lib().resist_dropout_backward(M, N, dt, dy.data_ptr(), _ld(dy), p, _rng_ptr(rng, p, dy), code, _opt(z),
-                                             _ld(z) if z is not None else 0, dx.data_ptr(), 0, on.ptr))
+    st = _on(dy, stream)
+    if st is None:
+        return _there(dropout_backward, stream, dy, p, rng, act, z)
+    dt, code = _dtype_of(dy), _activation(act)
+    dy = _matrix(dy, "dy")
+    M, N = dy.shape
+    if code and z is None:
+        raise ResistError("z: needed for the gradient of an activation")
+    z = _matrix(z, "z", dy, (M, N)) if code else None
+    dx = dy.new_empty((M, N))
+    _check(lib().resist_dropout_backward(M, N, dt, dy.data_ptr(), _ld(dy), p, _rng_ptr(rng, p, dy), code, _opt(z), _ld(z), dx.data_ptr(), 0, st))
     return dx
 
 
-def _linear_ws(shape, op, device):
-    import torch
+@functools.lru_cache(maxsize=4096)
+def _linear_ws_bytes(M, K, N, ldx, ldy, dt, op):
     n = C.c_int64()
-    _check(lib().resist_linear_workspace_bytes(C.byref(shape), op, C.byref(n)))
-    return (torch.empty(n.value, dtype=torch.uint8, device=device) if n.value else None), n.value
+    _check(lib().resist_linear_workspace_bytes(C.byref(_LinearShape(M, K, N, ldx, ldy, dt)), op, C.byref(n)))
+    return n.value
+
+
+def _linear_ws(like, op, *shape):
+    """-> (workspace or None, its bytes)."""
+    n = _linear_ws_bytes(*shape, op)
+    if not n:
+        return None, 0
+    import torch
+    return like.new_empty(n, dtype=torch.uint8), n
 
 
 def _weights(w, like, K=None, N=None):
@@ -663,62 +695,63 @@ def _weights(w, like, K=None, N=None):
 def linear_forward(x, w, bias=None, act="none", p=0.0, rng=None, residual=None, keep_z=False, stream=None):
     """[residual +] dropout(act(x w' + bias)): x [M, K] and w [N, K] of one dtype, bias [N] float32 or None, residual [M, N] or None;
     dropout as in dropout_forward -> y [M, N], with keep_z (y, z), z = x w' + bias as the gradients need it."""
-    import torch
-    with _On(x, stream) as on:
-        dt, code = _dtype_code(x), _activation(act)
-        x = _matrix(x, "x")
-        M, K = x.shape
-        w = _weights(w, x, K=K)
-        N = w.shape[0]
-        bias = _vector(bias, "bias", N, x)
-        residual = _matrix(residual, "residual", x, (M, N)) if residual is not None else None
-        on.uses(x, w, bias, rng, residual)
-        y = torch.empty((M, N), dtype=x.dtype, device=on.device)
-        z = torch.empty((M, N), dtype=x.dtype, device=on.device) if keep_z else None
-        sh = _LinearShape(M, K, N, _ld(x), 0, dt)
-        e = _LinearEpilogue(_opt(bias), code, p, _rng_ptr(rng, p, x), _opt(residual), _ld(residual) if residual is not None else 0, _opt(z), 0)
-        ws, n = _linear_ws(sh, 0, on.device)
-        _check(lib().resist_linear_forward(C.byref(sh), x.data_ptr(), w.data_ptr(), C.byref(e), y.data_ptr(), _opt(ws), n, on.ptr))
+    st = _on(x, stream)
+    if st is None:
+        return _there(linear_forward, stream, x, w, bias, act, p, rng, residual, keep_z)
+    dt, code = _dtype_of(x), _activation(act)
+    x = _matrix(x, "x")
+    M, K = x.shape
+    w = _weights(w, x, K=K)
+    N = w.shape[0]
+    bias = _vector(bias, "bias", N, x)
+    residual = _matrix(residual, "residual", x, (M, N)) if residual is not None else None
+    y = x.new_empty((M, N))
+    z = x.new_empty((M, N)) if keep_z else None
+    ldx = _ld(x)
+    ws, n = _linear_ws(x, 0, M, K, N, ldx, 0, dt)
+    _check(lib().resist_linear_forward(_LinearShape(M, K, N, ldx, 0, dt), x.data_ptr(), w.data_ptr(),
+                                       _LinearEpilogue(_opt(bias), code, p, _rng_ptr(rng, p, x), _opt(residual), _ld(residual), _opt(z), 0),
+                                       y.data_ptr(), _opt(ws), n, st))
     return (y, z) if keep_z else y
 
 
 def linear_dgrad(dz, w, act="none", z=None, p=0.0, rng=None, stream=None):
     """Gradient with respect to the input of a dense layer, dz w, dz [M, N], w [N, K] -- taken on, where that input was dropout(act(z)) with
     z [M, K], through this dropout and activation to the gradient with respect to z."""
-    import torch
-    with _On(dz, stream) as on:
-        dt, code = _dtype_code(dz), _activation(act)
-        dz = _matrix(dz, "dz")
-        M, N = dz.shape
-        w = _weights(w, dz, N=N)
-        K = w.shape[1]
-        if code and z is None:
-            raise ResistError("z: needed for the gradient of an activation")
-        z = _matrix(z, "z", dz, (M, K)) if code else None
-        on.uses(dz, w, z, rng)
-        dx = torch.empty((M, K), dtype=dz.dtype, device=on.device)
-        sh = _LinearShape(M, K, N, 0, _ld(dz), dt)
-        t = _LinearThrough(code, _opt(z), _ld(z) if z is not None else 0, p, _rng_ptr(rng, p, dz))
-        ws, n = _linear_ws(sh, 1, on.device)
-        _check(lib().resist_linear_dgrad(C.byref(sh), dz.data_ptr(), w.data_ptr(), C.byref(t), dx.data_ptr(), _opt(ws), n, on.ptr))
+    st = _on(dz, stream)
+    if st is None:
+        return _there(linear_dgrad, stream, dz, w, act, z, p, rng)
+    dt, code = _dtype_of(dz), _activation(act)
+    dz = _matrix(dz, "dz")
+    M, N = dz.shape
+    w = _weights(w, dz, N=N)
+    K = w.shape[1]
+    if code and z is None:
+        raise ResistError("z: needed for the gradient of an activation")
+    z = _matrix(z, "z", dz, (M, K)) if code else None
+    dx = dz.new_empty((M, K))
+    ldy = _ld(dz)
+    ws, n = _linear_ws(dz, 1, M, K, N, 0, ldy, dt)
+    _check(lib().resist_linear_dgrad(_LinearShape(M, K, N, 0, ldy, dt), dz.data_ptr(), w.data_ptr(),
+                                     _LinearThrough(code, _opt(z), _ld(z), p, _rng_ptr(rng, p, dz)), dx.data_ptr(), _opt(ws), n, st))
     return dx
 
 
 def linear_wgrad(dz, x, stream=None):
     """Gradients of a dense layer's parameters: dz [M, N], x [M, K] -> (dw [N, K], db [N]), float32."""
+    st = _on(dz, stream)
+    if st is None:
+        return _there(linear_wgrad, stream, dz, x)
     import torch
-    with _On(x, stream) as on:
-        dt = _dtype_code(x)
-        x = _matrix(x, "x")
-        M, K = x.shape
-        dz = _matrix(dz, "dz", x)
-        if dz.shape[0] != M:
-            raise ResistError(f"dz: {dz.shape[0]} rows beside {M} of x")
-        N = dz.shape[1]
-        on.uses(dz, x)
-        dw = torch.empty((N, K), dtype=torch.float32, device=on.device)
-        db = torch.empty(N, dtype=torch.float32, device=on.device)
-        sh = _LinearShape(M, K, N, _ld(x), _ld(dz), dt)
-        ws, n = _linear_ws(sh, 2, on.device)
-        _check(lib().resist_linear_wgrad(C.byref(sh), dz.data_ptr(), x.data_ptr(), dw.data_ptr(), db.data_ptr(), _opt(ws), n, on.ptr))
+    dt = _dtype_of(dz)
+    dz = _matrix(dz, "dz")
+    M, N = dz.shape
+    x = _matrix(x, "x", dz)
+    if x.shape[0] != M:
+        raise ResistError(f"x: {x.shape[0]} rows beside {M} of dz")
+    K = x.shape[1]
+    dw, db = dz.new_empty((N, K), dtype=torch.float32), dz.new_empty(N, dtype=torch.float32)
+    ldx, ldy = _ld(x), _ld(dz)
+    ws, n = _linear_ws(dz, 2, M, K, N, ldx, ldy, dt)
+    _check(lib().resist_linear_wgrad(_LinearShape(M, K, N, ldx, ldy, dt), dz.data_ptr(), x.data_ptr(), dw.data_ptr(), db.data_ptr(), _opt(ws), n, st))
     return dw, db

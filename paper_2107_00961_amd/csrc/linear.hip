@@ -2,7 +2,12 @@
 //   forward          z = x w' + bias,  y = residual + drop(a(z))
 //   data gradient    dx = a'(z) drop(dz w)        (z, a, drop: of the layer that produced x)
 //   weight gradient  dw = dz' x,  db = column sums of dz
-// Products on the matrix cores, sums in fp32, one rounding where a result is stored.
+// All three are one product, out(i, j) = sum over r of a(i, r) b(j, r), with either index contiguous in either operand.  Products on the matrix
+// cores, sums in fp32, one rounding where a result is stored.  Three ways:
+//   tiles      (gemm_tile_kernel) bf16 operands, or the three bf16 parts of fp32 ones (conv3.hip says why that loses nothing)
+//   few rows   (few_rows_kernel) the forward pass of up to 16 rows: w is read once, straight into fragments
+//   plain      (plain_tile) what of an fp32 product three parts do not hold, on the fp32 matrix instruction
+// Operands whose rows are not 16-byte aligned, and those in parts, are laid out in the workspace first (lay_out_kernel).
 #include <algorithm>
 
 #include "conv_tile.h"
@@ -25,16 +30,6 @@ struct Epilogue {
   int act, words;
 };
 
-// out(i, j) = sum over r of a(i, r) b(j, r); element (i, r) is a[i * ai + r * ar]
-struct GemmArgs {
-  const void *a, *b;
-  long long ai, ar, bj, br;
-  long long I;
-  int J, tiles_j;
-  long long R;
-  Epilogue e;
-};
-
 // element (i, j)
 template <typename T>
 __device__ inline void finish(const Epilogue &e, long long i, int j, float v, u64 base) {
@@ -54,66 +49,104 @@ __device__ inline void finish(const Epilogue &e, long long i, int j, float v, u6
   static_cast<T *>(e.out)[i * e.ldo + j] = (T)t[0];
 }
 
-// Any strides: 64x64 outputs to a workgroup, 32 steps of the reduction staged at a time, an element per load.  AR, BR: whether the
-// reduction index is the contiguous one.  T: operands, O: results.
-template <typename T, typename O, bool AR, bool BR>
-__global__ __launch_bounds__(kThreads) void gemm_any_kernel(GemmArgs g) {
-  using E = Elem<T>;
-  constexpr int BK = 32, PITCH = BK + E::VEC;
-  __shared__ __attribute__((aligned(16))) T As[64][PITCH], Bs[64][PITCH];
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, wm = wave >> 1, wn = wave & 1;
-  const int bid = blockIdx.x;
-  const long long i0 = (long long)(bid / g.tiles_j) * 64;
-  const int j0 = bid % g.tiles_j * 64;
-  const T *a = static_cast<const T *>(g.a), *b = static_cast<const T *>(g.b);
-  f32x16 acc = {};
-  for (long long r0 = 0; r0 < g.R; r0 += BK) {
+// ---- operands in the workspace --------------------------------------------------------------------------------------
+// A matrix [rows][n] with `ld` elements between rows becomes [rows][to_ld] of bf16, to_ld a multiple of eight, with zeros behind a row's end:
+// a copy (bf16), or three planes of parts (fp32).  Of parts, each 64x64 block also leaves a word: whether it has a value that three parts
+// do not hold (conv3.hip: not finite or rounding to infinity, or below 2^-110).
+struct LayOut {
+  const void *from;
+  __bf16 *to;
+  unsigned *flags;          // [ceil(rows/64)][ceil(to_ld/64)]
+  float *sums;              // optional [ceil(rows/64)][n]: of the columns, 64 rows each
+  long long rows, ld, plane;   // plane: elements between planes
+  int n, to_ld, blocks_n, blocks;
+};
+struct LayOutArgs { LayOut m[2]; };
+// split_check, and for NaN: what two parts leave of a value that is not finite or rounds to infinity
+__device__ inline void parts_check(const f32x4 &v, unsigned long long &missed) {
 #pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      const int i = AR ? tid >> 2 : tid & 63, r = AR ? (tid & 3) * 8 + e : (tid >> 6) * 8 + e;
-      As[i][r] = i0 + i < g.I && r0 + r < g.R ? a[(i0 + i) * g.ai + (r0 + r) * g.ar] : (T)0.f;
-      const int j = BR ? tid >> 2 : tid & 63, q = BR ? (tid & 3) * 8 + e : (tid >> 6) * 8 + e;
-      Bs[j][q] = j0 + j < g.J && r0 + q < g.R ? b[(j0 + j) * g.bj + (r0 + q) * g.br] : (T)0.f;
-    }
-    __syncthreads();
-#pragma unroll
-    for (int k = 0; k < BK; k += 2 * E::VEC) {
-      const f32x4 fa = *reinterpret_cast<const f32x4 *>(&As[wm * 32 + (lane & 31)][k + (lane >> 5) * E::VEC]);
-      const f32x4 fb = *reinterpret_cast<const f32x4 *>(&Bs[wn * 32 + (lane & 31)][k + (lane >> 5) * E::VEC]);
-      E::mma(acc, fa, fb);
-    }
-    __syncthreads();
+  for (int e = 0; e < 4; ++e) {
+    unsigned long long lanes;
+    asm("v_cmp_class_f32 %0, %1, %2" : "=s"(lanes) : "v"(v[e]), "s"(0x93));   // subnormal of either sign, NaN
+    missed |= lanes;
   }
-  const u64 base = g.e.d.rng ? dropout_base(g.e.d.rng) : 0;
-  const int j = j0 + wn * 32 + (lane & 31);
+}
+template <int NP>
+__global__ __launch_bounds__(kThreads) void lay_out_kernel(LayOutArgs a) {
+  using T = std::conditional_t<NP == 3, float, __bf16>;
+  const int second = (int)blockIdx.x >= a.m[0].blocks;
+  const LayOut &m = a.m[second];
+  const int b = blockIdx.x - (second ? a.m[0].blocks : 0);
+  const int bi = b / m.blocks_n, bj = b - bi * m.blocks_n;
+  const int c = bj * 64 + (threadIdx.x & 7) * 8;
+  unsigned long long missed = 0;
+  float sum[8] = {};
 #pragma unroll
-  for (int e = 0; e < 16; ++e) {
-    const long long i = i0 + wm * 32 + (e >> 2) * 8 + (lane >> 5) * 4 + (e & 3);
-    if (i < g.I && j < g.J) finish<O>(g.e, i, j, acc[e], base);
+  for (int p = 0; p < 2; ++p) {
+    const long long row = (long long)bi * 64 + p * 32 + (threadIdx.x >> 3);
+    if (row >= m.rows || c >= m.to_ld) continue;
+    float v[8];
+    row_load(static_cast<const T *>(m.from) + row * m.ld + c, m.n - c, v);
+    __bf16 *to = m.to + row * m.to_ld + c;
+    if constexpr (NP == 3) {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) sum[e] += v[e];
+      f32x4 lo = {v[0], v[1], v[2], v[3]}, hi = {v[4], v[5], v[6], v[7]};
+#pragma unroll
+      for (int q = 0; q < 3; ++q) {
+        if (q == 2) {
+          parts_check(lo, missed);
+          parts_check(hi, missed);
+        }
+        const u32x2 x = split_part(lo), y = split_part(hi);
+        *reinterpret_cast<u32x4 *>(to + q * m.plane) = u32x4{x[0], x[1], y[0], y[1]};
+      }
+    } else {
+      row_store(to, 8, v);
+    }
+  }
+  if constexpr (NP == 3) {
+    const int any = __syncthreads_or(missed != 0);
+    if (threadIdx.x == 0) m.flags[b] = any;
+    if (m.sums) {
+      __shared__ float cols[32][65];
+#pragma unroll
+      for (int e = 0; e < 8; ++e) cols[threadIdx.x >> 3][(threadIdx.x & 7) * 8 + e] = sum[e];
+      __syncthreads();
+      const int k = threadIdx.x;
+      if (k < 64 && bj * 64 + k < m.n) {
+        float t = 0.f;
+#pragma unroll
+        for (int r = 0; r < 32; ++r) t += cols[r][k];
+        m.sums[(size_t)bi * m.n + bj * 64 + k] = t;
+      }
+    }
   }
 }
 
-// ---- bf16 operands, tiled -------------------------------------------------------------------------------------------
+// ---- tiles --------------------------------------------------------------------------------------------
 // Operand tiles go from memory straight into LDS (16 bytes a lane, 1 KB a wave and instruction, in lane order), STAGES deep, and from there
 // in fragments to the matrix cores.  Four waves, a quarter of the BM x BN tile each: the larger a wave's share, the fewer times a
 // staged element is read from LDS (256x256: 1024 clocks of reading and 512 of arriving for 2048 of products).
 // Layout in LDS.  Lane order leaves no room for padding, so what keeps rows off each other's banks is which 16-byte piece a lane asks for:
 //   reduction contiguous (R): a row is an index i, BK values of r: piece c of row i lies at c ^ f(i), f = i & 7 (BK 64, 128 bytes a row),
 //     (i >> 1) & 3 (BK 32, two rows to 128 bytes): eight consecutive rows' pieces c fill 128 bytes;
-//   other index contiguous: a row is an r, BM values of i: piece c of row r lies at c ^ 4 (r & 3): the four rows of a transpose
-//     read, 64 bytes each, fill 256 bytes.
+//   other index contiguous: a row is an r, BM values of i: piece c of row r lies at c ^ 4 (r & 3) (64 values, two rows to 256 bytes:
+//     c ^ 2 (r & 2)): the four rows of a transpose read, 64 bytes each, fill 256 bytes.
 // Bounds: an operand's descriptor starts at the tile and ends with the operand (rows past it, and steps past it, come as zeros); its
 // contiguous axis is a multiple of eight where it is the reduction (a tail's pieces are not asked for) and may end in a piece where it is
 // not (what a tile has past its last column goes into outputs that are not stored).
+// Operands in three parts are three such tiles each, and a product is six (small ones first).
 template <bool R, int B, int BK> struct Stage {
-  static constexpr int kBytes = B * BK * 2, kLoads = kBytes / 4096;   // a wave's instructions
+  static constexpr int kBytes = B * BK * 2, kLoads = kBytes / 4096;   // of a plane; a wave's instructions
   static constexpr int kRow = R ? BK * 2 : B * 2, kPieces = kRow / 16, kRows = 1024 / kRow;   // rows an instruction
+  __device__ static inline int swizzle(int row) {
+    if (R) return BK == 64 ? row & 7 : (row >> 1) & 3;
+    return kPieces == 8 ? (row & 2) << 1 : (row & 3) << 2;
+  }
   // row and piece of the tile that lane `l` of wave `w` asks for with instruction p
   __device__ static inline int row(int p, int w, int l) { return (p * 4 + w) * kRows + l / kPieces; }
-  __device__ static inline int piece(int r, int l) {
-    const int f = R ? (BK == 64 ? r & 7 : (r >> 1) & 3) : (r & 3) << 2;
-    return (l % kPieces) ^ f;
-  }
+  __device__ static inline int piece(int r, int l) { return (l % kPieces) ^ swizzle(r); }
 };
 
 struct TileArgs {
@@ -124,6 +157,12 @@ struct TileArgs {
   int splits;
   long long per_split;      // steps of the reduction, a multiple of the tile's
   float *part;              // [splits][I][J] where the reduction is split
+  float *sums;              // optional (neither reduction contiguous): [splits * tiles_j * 2][I], parts of the sums of a over r
+  // operands in parts: elements between planes, the words of their blocks, and the operands themselves
+  long long plane_a, plane_b;
+  const unsigned *flags_a, *flags_b;
+  const float *a32, *b32;
+  long long lda32, ldb32;
   Epilogue e;
 };
 
@@ -174,12 +213,50 @@ __device__ inline void tile_of(int bid, int tiles_i, int tiles_j, int group, int
   ti = g * group + rest - tj * rows;
 }
 
-template <typename O, bool AR, bool BR, int BM, int BN, int BK, int STAGES, int WGS>
+// BM x BN outputs from the operands as they are, in fp32 on its own matrix instruction, 64x64 at a time: for operands and results that three parts do
+// not hold.  `lds`: 18 KB.  to(i, j, v) takes an output.
+template <bool AR, bool BR, int BM, int BN, typename To>
+__device__ inline void plain_tile(const TileArgs &g, long long i0, int j0, long long rbeg, long long rend, char *lds, To to) {
+  constexpr int BK = 32;
+  float (*As)[BK + 4] = reinterpret_cast<float (*)[BK + 4]>(lds), (*Bs)[BK + 4] = As + 64;
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, wm = wave >> 1, wn = wave & 1;
+  const long long ai = AR ? g.lda32 : 1, ar = AR ? 1 : g.lda32, bj = BR ? g.ldb32 : 1, br = BR ? 1 : g.ldb32;
+#pragma unroll 1
+  for (int s = 0; s < (BM / 64) * (BN / 64); ++s) {
+    const long long i1 = i0 + s / (BN / 64) * 64;
+    const int j1 = j0 + s % (BN / 64) * 64;
+    f32x16 acc = {};
+#pragma unroll 1
+    for (long long r0 = rbeg; r0 < rend; r0 += BK) {
+      __syncthreads();
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        const int i = AR ? tid >> 2 : tid & 63, r = AR ? (tid & 3) * 8 + e : (tid >> 6) * 8 + e;
+        As[i][r] = i1 + i < g.I && r0 + r < rend ? g.a32[(i1 + i) * ai + (r0 + r) * ar] : 0.f;
+        const int j = BR ? tid >> 2 : tid & 63, q = BR ? (tid & 3) * 8 + e : (tid >> 6) * 8 + e;
+        Bs[j][q] = j1 + j < g.J && r0 + q < rend ? g.b32[(j1 + j) * bj + (r0 + q) * br] : 0.f;
+      }
+      __syncthreads();
+#pragma unroll
+      for (int k = 0; k < BK; k += 8)
+        Elem<float>::mma(acc, *reinterpret_cast<const f32x4 *>(&As[wm * 32 + (lane & 31)][k + (lane >> 5) * 4]),
+                         *reinterpret_cast<const f32x4 *>(&Bs[wn * 32 + (lane & 31)][k + (lane >> 5) * 4]));
+    }
+    const int j = j1 + wn * 32 + (lane & 31);
+#pragma unroll
+    for (int e = 0; e < 16; ++e) {
+      const long long i = i1 + wm * 32 + (e >> 2) * 8 + (lane >> 5) * 4 + (e & 3);
+      if (i < g.I && j < g.J) to(i, j, acc[e]);
+    }
+  }
+}
+
+template <typename O, bool AR, bool BR, int NP, int BM, int BN, int BK, int STAGES, int WGS>
 __global__ __launch_bounds__(kThreads, WGS) void gemm_tile_kernel(TileArgs g) {
   using SA = Stage<AR, BM, BK>;
   using SB = Stage<BR, BN, BK>;
   constexpr int WTM = BM / 2, WTN = BN / 2, TM = WTM / 32, TN = WTN / 32, NK = BK / 16;
-  constexpr int kStage = SA::kBytes + SB::kBytes, kLoads = SA::kLoads + SB::kLoads;
+  constexpr int kLoadsA = NP * SA::kLoads, kLoads = kLoadsA + NP * SB::kLoads, kA = NP * SA::kBytes, kStage = kA + NP * SB::kBytes;
   constexpr int kPitch = WTN * 4 + 16, kOut = 4 * 2 * 32 * kPitch;
   static_assert(STAGES >= 2, "stages");
   static_assert(TM <= 4, "tile");
@@ -195,8 +272,8 @@ __global__ __launch_bounds__(kThreads, WGS) void gemm_tile_kernel(TileArgs g) {
   // ---- operands to LDS.  left: bytes from the tile's current corner to the operand's end
   const char *pa = reinterpret_cast<const char *>(g.a + (AR ? i0 * g.lda + rbeg : rbeg * g.lda + i0));
   const char *pb = reinterpret_cast<const char *>(g.b + (BR ? (long long)j0 * g.ldb + rbeg : rbeg * g.ldb + j0));
-  long long left_a = AR ? ((g.I - i0 - 1) * g.lda + (rend - rbeg)) * 2 : ((rend - rbeg - 1) * g.lda + (g.I - i0 + 7) / 8 * 8) * 2;
-  long long left_b = BR ? ((g.J - j0 - 1) * g.ldb + (rend - rbeg)) * 2 : ((rend - rbeg - 1) * g.ldb + (g.J - j0 + 7) / 8 * 8) * 2;
+  long long left_a = AR ? ((g.I - i0 - 1) * g.lda + (rend - rbeg + 7) / 8 * 8) * 2 : ((rend - rbeg - 1) * g.lda + (g.I - i0 + 7) / 8 * 8) * 2;
+  long long left_b = BR ? ((g.J - j0 - 1) * g.ldb + (rend - rbeg + 7) / 8 * 8) * 2 : ((rend - rbeg - 1) * g.ldb + (g.J - j0 + 7) / 8 * 8) * 2;
   unsigned va[SA::kLoads], vb[SB::kLoads];
 #pragma unroll
   for (int p = 0; p < SA::kLoads; ++p) {
@@ -213,12 +290,13 @@ __global__ __launch_bounds__(kThreads, WGS) void gemm_tile_kernel(TileArgs g) {
   int left_r = (int)min(rend - rbeg, (long long)0x40000000);
   const unsigned lds_at = __builtin_amdgcn_readfirstlane((unsigned)(uintptr_t)(__attribute__((address_space(3))) char *)lds) + wave * 1024;
   auto request = [&](int p, int stage) {   // instruction p of the step
-    const bool is_a = p < SA::kLoads;
-    const __amdgpu_buffer_rsrc_t r = is_a ? make_rsrc(pa, left_a > 0 ? (unsigned)min(left_a, 0x7ffffff0LL) : 0u)
-                                          : make_rsrc(pb, left_b > 0 ? (unsigned)min(left_b, 0x7ffffff0LL) : 0u);
-    unsigned v = is_a ? va[p] : vb[p - SA::kLoads];
+    const bool is_a = p < kLoadsA;
+    const int q = is_a ? p : p - kLoadsA, per = is_a ? SA::kLoads : SB::kLoads, plane = q / per;
+    const __amdgpu_buffer_rsrc_t r = is_a ? make_rsrc(pa + plane * g.plane_a * 2, left_a > 0 ? (unsigned)min(left_a, 0x7ffffff0LL) : 0u)
+                                          : make_rsrc(pb + plane * g.plane_b * 2, left_b > 0 ? (unsigned)min(left_b, 0x7ffffff0LL) : 0u);
+    unsigned v = is_a ? va[q % per] : vb[q % per];
     if (is_a ? AR : BR) v = (is_a ? ka : kb) < left_r ? v : kOOB;
-    transfer(r, v, lds_at + stage * kStage + (is_a ? p * 4096 : SA::kBytes + (p - SA::kLoads) * 4096));
+    transfer(r, v, lds_at + stage * kStage + (is_a ? 0 : kA) + q * 4096);
   };
   auto advance = [&]() {
     const long long da = (AR ? BK : BK * g.lda) * 2, db = (BR ? BK : BK * g.ldb) * 2;
@@ -232,37 +310,39 @@ __global__ __launch_bounds__(kThreads, WGS) void gemm_tile_kernel(TileArgs g) {
   int oa[AR ? NK : TM], ob[BR ? NK : TN];
   if constexpr (AR) {
 #pragma unroll
-    for (int k = 0; k < NK; ++k) oa[k] = (wm * WTM + lr) * SA::kRow + (((k * 2 + lg) ^ (BK == 64 ? lr & 7 : (lr >> 1) & 3)) << 4);
+    for (int k = 0; k < NK; ++k) oa[k] = (wm * WTM + lr) * SA::kRow + (((k * 2 + lg) ^ SA::swizzle(lr)) << 4);
   } else {
     const int fr = lg * 8 + ((lane & 15) >> 2), fc = ((lane >> 4) & 1) * 16 + (lane & 3) * 4;
 #pragma unroll
     for (int i = 0; i < TM; ++i) {
       const int c = wm * WTM + i * 32 + fc;
-      oa[i] = fr * SA::kRow + (((c >> 3) ^ ((fr & 3) << 2)) << 4) + (c & 7) * 2;
+      oa[i] = fr * SA::kRow + (((c >> 3) ^ SA::swizzle(fr)) << 4) + (c & 7) * 2;
     }
   }
   if constexpr (BR) {
 #pragma unroll
-    for (int k = 0; k < NK; ++k) ob[k] = (wn * WTN + lr) * SB::kRow + (((k * 2 + lg) ^ (BK == 64 ? lr & 7 : (lr >> 1) & 3)) << 4);
+    for (int k = 0; k < NK; ++k) ob[k] = (wn * WTN + lr) * SB::kRow + (((k * 2 + lg) ^ SB::swizzle(lr)) << 4);
   } else {
     const int fr = lg * 8 + ((lane & 15) >> 2), fc = ((lane >> 4) & 1) * 16 + (lane & 3) * 4;
 #pragma unroll
     for (int j = 0; j < TN; ++j) {
       const int c = wn * WTN + j * 32 + fc;
-      ob[j] = fr * SB::kRow + (((c >> 3) ^ ((fr & 3) << 2)) << 4) + (c & 7) * 2;
+      ob[j] = fr * SB::kRow + (((c >> 3) ^ SB::swizzle(fr)) << 4) + (c & 7) * 2;
     }
   }
-  bf16x8 fa[2][TM], fb[2][TN];
-  auto fetch = [&](int n, int set, int stage, int k) {   // fragment n, in the order the products want them: A's first, B's, the rest of A's
-    const char *A = lds + stage * kStage, *B = A + SA::kBytes;
-    if (n == 0 || n > TN) {
-      const int i = n == 0 ? 0 : n - TN;
-      if constexpr (AR) fa[set][i] = *reinterpret_cast<const bf16x8 *>(A + oa[k] + i * 32 * SA::kRow);
-      else fa[set][i] = lds_read_tr_pair(A + oa[i] + k * 16 * SA::kRow, A + oa[i] + (k * 16 + 4) * SA::kRow);
+  bf16x8 fa[2][NP][TM], fb[2][NP][TN];
+  constexpr int kFrags = NP * (TM + TN);
+  auto fetch = [&](int n, int set, int stage, int k) {   // fragment n, plane by plane from the smallest part on, of a plane A's first, B's, the rest of A's
+    const int p = NP - 1 - n / (TM + TN), m = n % (TM + TN);
+    const char *A = lds + stage * kStage + p * SA::kBytes, *B = lds + stage * kStage + kA + p * SB::kBytes;
+    if (m == 0 || m > TN) {
+      const int i = m == 0 ? 0 : m - TN;
+      if constexpr (AR) fa[set][p][i] = *reinterpret_cast<const bf16x8 *>(A + oa[k] + i * 32 * SA::kRow);
+      else fa[set][p][i] = lds_read_tr_pair(A + oa[i] + k * 16 * SA::kRow, A + oa[i] + (k * 16 + 4) * SA::kRow);
     } else {
-      const int j = n - 1;
-      if constexpr (BR) fb[set][j] = *reinterpret_cast<const bf16x8 *>(B + ob[k] + j * 32 * SB::kRow);
-      else fb[set][j] = lds_read_tr_pair(B + ob[j] + k * 16 * SB::kRow, B + ob[j] + (k * 16 + 4) * SB::kRow);
+      const int j = m - 1;
+      if constexpr (BR) fb[set][p][j] = *reinterpret_cast<const bf16x8 *>(B + ob[k] + j * 32 * SB::kRow);
+      else fb[set][p][j] = lds_read_tr_pair(B + ob[j] + k * 16 * SB::kRow, B + ob[j] + (k * 16 + 4) * SB::kRow);
     }
   };
 
@@ -288,11 +368,15 @@ __global__ __launch_bounds__(kThreads, WGS) void gemm_tile_kernel(TileArgs g) {
   for (int p = 0; p < kEach; ++p) request(p, STAGES - 1);
   wait_and_meet<(STAGES - 2) * kLoads + kEach>();
 #pragma unroll
-  for (int n = 0; n < TM + TN; ++n) fetch(n, 0, 0, 0);
+  for (int n = 0; n < kFrags; ++n) fetch(n, 0, 0, 0);
   __builtin_amdgcn_sched_barrier(0);
   int stage = 0, refill = STAGES - 1;
-  auto step = [&](auto kc, int next) {
-    constexpr int k = decltype(kc)::value, MF = TM * TN, DS = TM + TN, MD = MF * 3 / 4;
+  // sums of a over r (the gradient of a bias): of the steps t with t % tiles_j == tj, the first waves in the even, the second in the odd products
+  constexpr bool kSums = !AR && NP == 1;
+  float sums[TM] = {};
+  int sums_at = kSums && g.sums ? tj : 0x7fffffff;
+  auto step = [&](auto kc, int next, bool take) {
+    constexpr int k = decltype(kc)::value, PAIRS = NP == 3 ? 6 : 1, MF = PAIRS * TM * TN, MD = MF > 1 ? MF * 3 / 4 : 1, MH = MF > 1 ? MF / 2 : 1;
     constexpr bool last = k + 1 == NK;
     if constexpr (last) {
       advance();
@@ -301,22 +385,34 @@ __global__ __launch_bounds__(kThreads, WGS) void gemm_tile_kernel(TileArgs g) {
     int ds = 0, vm = 0;
 #pragma unroll
     for (int m = 0; m < MF; ++m) {   // a product, then what goes on beside it, in this order
-      const int i = m / TN, j = m % TN;
-      acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fb[k & 1][j], fa[k & 1][i], acc[i][j], 0, 0, 0);
+      const int pair = m / (TM * TN), i = m / TN % TM, j = m % TN;
+      const int pa_ = NP == 1 ? 0 : pair == 0 ? 2 : pair == 1 ? 0 : pair == 2 ? 1 : pair == 3 ? 1 : 0;   // parts l h', h l', m m', m h', h m', h h'
+      const int pb_ = NP == 1 ? 0 : pair == 0 ? 0 : pair == 1 ? 2 : pair == 2 ? 1 : pair == 3 ? 0 : pair == 4 ? 1 : 0;
+      acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fb[k & 1][pb_][j], fa[k & 1][pa_][i], acc[i][j], 0, 0, 0);
 #pragma unroll
-      for (; ds < (m < MD ? (m + 1) * DS / MD : DS); ++ds) fetch(ds, (k + 1) & 1, last ? next : stage, last ? 0 : k + 1);
+      for (; ds < (m + 1 < MD ? (m + 1) * kFrags / MD : kFrags); ++ds) fetch(ds, (k + 1) & 1, last ? next : stage, last ? 0 : k + 1);
 #pragma unroll
-      for (; vm < (m < MF / 2 ? (m + 1) * kEach / (MF / 2) : kEach); ++vm) request(last ? vm : (k + 1) * kEach + vm, last ? stage : refill);
+      for (; vm < (m + 1 < MH ? (m + 1) * kEach / MH : kEach); ++vm) request(last ? vm : (k + 1) * kEach + vm, last ? stage : refill);
       __builtin_amdgcn_sched_barrier(0);
+    }
+    if constexpr (kSums) {
+      if (take && (k & 1) == wn) {
+#pragma unroll
+        for (int i = 0; i < TM; ++i)
+#pragma unroll
+          for (int e = 0; e < 8; ++e) sums[i] += (float)fa[k & 1][0][i][e];
+      }
     }
   };
   for (int t = 0; t < steps; ++t) {
     const int next = stage + 1 == STAGES ? 0 : stage + 1;
-    step(std::integral_constant<int, 0>{}, next);
-    step(std::integral_constant<int, 1>{}, next);
+    const bool take = kSums && t == sums_at;
+    if (take) sums_at += g.tiles_j;
+    step(std::integral_constant<int, 0>{}, next, take);
+    step(std::integral_constant<int, 1>{}, next, take);
     if constexpr (NK > 2) {
-      step(std::integral_constant<int, 2>{}, next);
-      step(std::integral_constant<int, 3>{}, next);
+      step(std::integral_constant<int, 2>{}, next, take);
+      step(std::integral_constant<int, 3>{}, next, take);
     }
     refill = stage;
     stage = next;
@@ -326,6 +422,46 @@ __global__ __launch_bounds__(kThreads, WGS) void gemm_tile_kernel(TileArgs g) {
   // wait behind but its own next rows: they are on their way from LDS, what the epilogue reads beside them for the next kAhead passes from
   // memory, while a pass is worked on.  One copy of the code (it is long, and the instruction cache is shared).
   asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");   // the steps past the end have arrived too
+  if constexpr (kSums) {
+    if (g.sums) {
+      float *to = g.sums + ((size_t)(split * g.tiles_j + tj) * 2 + wn) * g.I;
+#pragma unroll
+      for (int i = 0; i < TM; ++i) {
+        const float s = sums[i] + __shfl_xor(sums[i], 32, 64);
+        const long long at = i0 + wm * WTM + i * 32 + lr;
+        if (lg == 0 && at < g.I) to[at] = s;
+      }
+    }
+  }
+  if constexpr (NP == 3) {
+    int bad = 0;
+#pragma unroll
+    for (int i = 0; i < TM; ++i)
+#pragma unroll
+      for (int j = 0; j < TN; ++j)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) bad |= !(fabsf(acc[i][j][e]) <= 3.4028234e38f);
+    // the blocks of 64x64 whose values went into this tile
+    const int r0 = (int)(rbeg >> 6), r1 = (int)((rend + 63) >> 6), nr = r1 - r0, wide_a = AR ? (int)((g.R + 63) >> 6) : (int)((g.I + 63) >> 6),
+              wide_b = BR ? (int)((g.R + 63) >> 6) : (g.J + 63) >> 6;
+    const int ia = (int)(i0 >> 6), na = (int)min((long long)BM / 64, ((g.I + 63) >> 6) - ia), jb = j0 >> 6, nb = min(BN / 64, ((g.J + 63) >> 6) - jb);
+    for (int u = tid; u < nr * na; u += kThreads) {
+      const int r = r0 + u / na, i = ia + u % na;
+      bad |= g.flags_a[AR ? (size_t)i * wide_a + r : (size_t)r * wide_a + i];
+    }
+    for (int u = tid; u < nr * nb; u += kThreads) {
+      const int r = r0 + u / nb, j = jb + u % nb;
+      bad |= g.flags_b[BR ? (size_t)j * wide_b + r : (size_t)r * wide_b + j];
+    }
+    if (__syncthreads_or(bad)) {
+      const u64 base = g.e.d.rng && g.splits == 1 ? dropout_base(g.e.d.rng) : 0;
+      plain_tile<AR, BR, BM, BN>(g, i0, j0, rbeg, rend, lds, [&](long long i, int j, float v) {
+        if (g.splits > 1) g.part[((long long)split * g.I + i) * g.J + j] = v;
+        else finish<O>(g.e, i, j, v, base);
+      });
+      return;
+    }
+  }
   char *const mine = lds + wave * 2 * 32 * kPitch;
   const bool whole = g.splits == 1;
   const u64 base = g.e.d.rng && whole ? dropout_base(g.e.d.rng) : 0;
@@ -386,32 +522,113 @@ __global__ __launch_bounds__(kThreads, WGS) void gemm_tile_kernel(TileArgs g) {
   }
 }
 
-// the parts of a split reduction, in order
+// What follows a split reduction and the sums of columns: workgroups 0 .. sum_wgs-1 join `sum_parts` rows of sums of 64 columns each, in float64,
+// the others the parts of eight outputs a thread; in order.
+struct JoinArgs {
+  const float *part, *sums;
+  float *db;
+  long long I;
+  int splits, J, sum_parts, sum_n, sum_wgs;
+  Epilogue e;
+};
 template <typename O>
-__global__ __launch_bounds__(kThreads) void gemm_join_kernel(const float *part, int splits, long long I, int J, Epilogue e) {
-  const int nvec = (J + 7) / 8;
-  const long long u = (long long)blockIdx.x * kThreads + threadIdx.x;
+__global__ __launch_bounds__(kThreads) void gemm_join_kernel(JoinArgs a) {
+  if ((int)blockIdx.x < a.sum_wgs) {
+    __shared__ double red[4][64];
+    const int c = blockIdx.x * 64 + (threadIdx.x & 63), k = threadIdx.x >> 6;
+    double s = 0.;
+    if (c < a.sum_n)
+      for (int p = k; p < a.sum_parts; p += 4) s += (double)a.sums[(size_t)p * a.sum_n + c];
+    red[k][threadIdx.x & 63] = s;
+    __syncthreads();
+    if (k == 0 && c < a.sum_n) a.db[c] = (float)(((red[0][threadIdx.x] + red[1][threadIdx.x]) + red[2][threadIdx.x]) + red[3][threadIdx.x]);
+    return;
+  }
+  const int nvec = (a.J + 7) / 8;
+  const long long u = (long long)(blockIdx.x - a.sum_wgs) * kThreads + threadIdx.x;
   const long long row = u / nvec;
-  const int j = (int)(u - row * nvec) * 8, left = J - j;
-  if (row >= I) return;
+  const int j = (int)(u - row * nvec) * 8, left = a.J - j;
+  if (row >= a.I) return;
+  float bias[8];
+  bias_of(a.e, j, left, bias);
+  long long ld;
+  const O *side = side_of<O>(a.e, ld);
+  Raw8<O> now = {};
+  if (side) raw_load(side + row * ld + j, left, now);
   float v[8];
-  row_load(part + row * J + j, left, v);
-  for (int s = 1; s < splits; ++s) {
+  row_load(a.part + row * a.J + j, left, v);
+  for (int s = 1; s < a.splits; ++s) {
     float w[8];
-    row_load(part + ((long long)s * I + row) * J + j, left, w);
+    row_load(a.part + ((long long)s * a.I + row) * a.J + j, left, w);
 #pragma unroll
     for (int k = 0; k < 8; ++k) v[k] += w[k];
   }
-  float bias[8];
-  bias_of(e, j, left, bias);
-  long long ld;
-  const O *side = side_of<O>(e, ld);
-  Raw8<O> now = {};
-  if (side) raw_load(side + row * ld + j, left, now);
-  finish8<O>(e, row, j, left, v, bias, now, e.d.rng ? dropout_base(e.d.rng) : 0);
+  finish8<O>(a.e, row, j, left, v, bias, now, a.e.d.rng ? dropout_base(a.e.d.rng) : 0);
 }
 
-// db: 64 columns of dz to a workgroup, four ranges of rows
+// ---- few rows -------------------------------------------------------------------------------------------------------
+// y = x w' for at most 16 rows: the time is that of reading w once.  A workgroup takes 16 rows of w, its eight waves every eighth piece of the
+// reduction; fragments of both operands come straight from memory (rows that start anywhere are fine), several in flight, and the waves'
+// sums are joined in LDS, in order.
+struct FewArgs {
+  const void *x, *w;
+  long long ldx;
+  int M, K, N;
+  Epilogue e;
+};
+template <typename T>
+__global__ __launch_bounds__(512) void few_rows_kernel(FewArgs a) {
+  constexpr int V = 16 / (int)sizeof(T), STEP = 4 * V, AHEAD = 4;   // elements a lane, of the reduction a wave and load; loads in flight
+  __shared__ float red[8][16][17];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, row = lane & 15, kk = (lane >> 4) * V;
+  const int n = blockIdx.x * 16 + row;
+  const T *w = static_cast<const T *>(a.w) + (long long)(n < a.N ? n : 0) * a.K, *x = static_cast<const T *>(a.x) + (row < a.M ? row : 0) * a.ldx;
+  f32x4 acc = {};
+  typedef std::conditional_t<sizeof(T) == 4, f32x4, u32x4> Piece;
+  auto piece = [&](const T *p, int k, bool ok, Piece &out) {   // V elements from k on, zeros past the end
+    out = Piece{};
+    if (!ok || k >= a.K) return;
+    if (k + V <= a.K) {
+      if constexpr (sizeof(T) == 4) out = *reinterpret_cast<const f32x4_any *>(p + k);
+      else out = *reinterpret_cast<const u32x4_any *>(p + k);
+    } else {
+#pragma unroll
+      for (int e = 0; e < V; ++e)
+        if (k + e < a.K) {
+          if constexpr (sizeof(T) == 4) out[e] = p[k + e];
+          else out[e >> 1] |= (unsigned)__builtin_bit_cast(unsigned short, p[k + e]) << (e & 1 ? 16 : 0);
+        }
+    }
+  };
+  for (int k0 = wave * STEP; k0 < a.K; k0 += 8 * STEP * AHEAD) {
+    Piece fw[AHEAD], fx[AHEAD];
+#pragma unroll
+    for (int u = 0; u < AHEAD; ++u) {
+      piece(w, k0 + u * 8 * STEP + kk, n < a.N, fw[u]);
+      piece(x, k0 + u * 8 * STEP + kk, row < a.M, fx[u]);
+    }
+#pragma unroll
+    for (int u = 0; u < AHEAD; ++u) {
+      if constexpr (sizeof(T) == 4) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) acc = __builtin_amdgcn_mfma_f32_16x16x4f32(fw[u][e], fx[u][e], acc, 0, 0, 0);
+      } else {
+        acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, fw[u]), __builtin_bit_cast(bf16x8, fx[u]), acc, 0, 0, 0);
+      }
+    }
+  }
+#pragma unroll
+  for (int e = 0; e < 4; ++e) red[wave][row][(lane >> 4) * 4 + e] = acc[e];   // lane: row `row` of x, four columns
+  __syncthreads();
+  const int m = threadIdx.x >> 4, c = threadIdx.x & 15, j = blockIdx.x * 16 + c;
+  if (threadIdx.x >= 256 || m >= a.M || j >= a.N) return;
+  float v = red[0][m][c];
+#pragma unroll
+  for (int s = 1; s < 8; ++s) v += red[s][m][c];
+  finish<T>(a.e, m, j, v, a.e.d.rng ? dropout_base(a.e.d.rng) : 0);
+}
+
+// db on its own: 64 columns of dz to a workgroup, four ranges of rows
 template <typename T>
 __global__ __launch_bounds__(kThreads) void col_sum_kernel(const T *dz, long long M, int N, long long ld, float *db) {
   __shared__ double red[4][64];
@@ -424,85 +641,220 @@ __global__ __launch_bounds__(kThreads) void col_sum_kernel(const T *dz, long lon
   if (k == 0 && c < N) db[c] = (float)(((red[0][threadIdx.x] + red[1][threadIdx.x]) + red[2][threadIdx.x]) + red[3][threadIdx.x]);
 }
 
-template <typename T, typename O, bool AR, bool BR> int gemm_any(GemmArgs &g, hipStream_t st) {
-  g.tiles_j = (g.J + 63) / 64;
-  const long long tiles = (g.I + 63) / 64 * g.tiles_j;
-  if (tiles > 0x7fffffffLL) return set_error(RESIST_ESHAPE, "linear: too many outputs");
-  gemm_any_kernel<T, O, AR, BR><<<(unsigned)tiles, kThreads, 0, st>>>(g);
+// ---- plans ----------------------------------------------------------------------------------------------------------
+constexpr int kFewRows = 16;
+
+struct Plan {
+  int size;                  // of the tiles: 0 the largest ... 2 the smallest
+  int bm, bn, splits;
+  long long per_split;
+};
+#ifndef RESIST_PLAN
+#define RESIST_PLAN -1, 0
+#endif
+constexpr int kForce[2] = {RESIST_PLAN};
+Plan plan_tiles(int np, long long I, long long J, long long R) {
+  static const int bm[2][3] = {{256, 128, 64}, {256, 128, 64}}, bn[2][3] = {{256, 128, 64}, {128, 128, 64}};
+  const int f = np == 3;
+  Plan p{};
+  p.size = I * J >= 256LL * 256 * 128 ? 0 : I * J >= 128 * 128 * 64 ? 1 : 2;
+  if (kForce[0] >= 0) p.size = kForce[0];
+  p.bm = bm[f][p.size]; p.bn = bn[f][p.size];
+  p.splits = 1;
+  if (kForce[1] > 0) p.splits = kForce[1];
+  const long long steps = (R + 63) / 64;
+  p.splits = (int)std::min<long long>(p.splits, steps);
+  p.per_split = (steps + p.splits - 1) / p.splits * 64;
+  p.splits = (int)((R + p.per_split - 1) / p.per_split);
+  return p;
+}
+
+// An operand of a call: `rows` rows of n elements; whether it has to be laid out, and where.
+struct Operand {
+  long long rows, ld;
+  int n;
+  bool moved;
+  long long to_ld, plane;    // as the kernel reads it
+  int64_t at, flags_at;      // bytes into the workspace
+};
+struct Layout {
+  Operand a, b;
+  int np;
+  Plan plan;
+  int64_t part_at, sums_at, bytes;
+  int sum_parts;
+};
+int64_t align256(int64_t n) { return (n + 255) & ~(int64_t)255; }
+int64_t blocks64(long long rows, long long n) { return ((rows + 63) / 64) * ((n + 63) / 64); }
+// `whole`: the reduction is the contiguous axis, so that a row's end has to be one of eight elements
+Operand operand(int dt, long long rows, int n, long long ld, bool whole, int64_t *at) {
+  Operand o{rows, ld, n, false, ld, 0, 0, 0};
+  o.moved = dt == DT_F32 || ld % 8 != 0 || (whole && n % 8 != 0);
+  if (!o.moved) return o;
+  o.to_ld = (n + 7) / 8 * 8;
+  o.plane = rows * o.to_ld;
+  o.at = *at;
+  *at += align256(o.plane * 2 * (dt == DT_F32 ? 3 : 1));
+  if (dt == DT_F32) {
+    o.flags_at = *at;
+    *at += align256(blocks64(rows, n) * 4);
+  }
+  return o;
+}
+// op 0 forward, 1 data gradient, 2 weight gradient
+Layout layout_of(const LinearShape &s, int dt, int op) {
+  Layout l{};
+  l.np = dt == DT_F32 ? 3 : 1;
+  const long long I = op == 2 ? s.N : s.M, J = op == 0 ? s.N : s.K, R = op == 0 ? s.K : op == 1 ? s.N : s.M;
+  l.plan = plan_tiles(l.np, I, J, R);
+  int64_t at = 0;
+  if (op == 0) {
+    l.a = operand(dt, s.M, s.K, s.ldx, true, &at);
+    l.b = operand(dt, s.N, s.K, s.K, true, &at);
+  } else if (op == 1) {
+    l.a = operand(dt, s.M, s.N, s.ldy, true, &at);
+    l.b = operand(dt, s.N, s.K, s.K, false, &at);
+  } else {
+    l.a = operand(dt, s.M, s.N, s.ldy, false, &at);
+    l.b = operand(dt, s.M, s.K, s.ldx, false, &at);
+  }
+  l.part_at = at;
+  if (l.plan.splits > 1) at += align256(l.plan.splits * I * J * 4);
+  if (op == 2) {
+    l.sums_at = at;
+    l.sum_parts = dt == DT_F32 ? (int)((s.M + 63) / 64) : (int)((J + l.plan.bn - 1) / l.plan.bn) * l.plan.splits * 2;
+    at += align256((int64_t)l.sum_parts * s.N * 4);
+  }
+  l.bytes = at;
+  return l;
+}
+
+template <typename O, bool AR, bool BR, int NP, int BM, int BN, int BK, int STAGES, int WGS> int launch_tiles(TileArgs &t, hipStream_t st) {
+  t.tiles_i = (int)((t.I + BM - 1) / BM);
+  t.tiles_j = (t.J + BN - 1) / BN;
+  t.group = 8;
+  const long long wgs = (long long)t.tiles_i * t.tiles_j * t.splits;
+  if (wgs > 0x7fffffffLL) return set_error(RESIST_ESHAPE, "linear: too many outputs");
+  gemm_tile_kernel<O, AR, BR, NP, BM, BN, BK, STAGES, WGS><<<(unsigned)wgs, kThreads, 0, st>>>(t);
   RESIST_CHECK_LAUNCH("linear");
   return RESIST_OK;
 }
 
-template <typename O, bool AR, bool BR, int BM, int BN, int BK, int STAGES, int WGS> int gemm_tiles_of(TileArgs &t, hipStream_t st) {
-  t.tiles_i = (int)((t.I + BM - 1) / BM);
-  t.tiles_j = (int)((t.J + BN - 1) / BN);
-  t.group = 8; t.splits = 1; t.per_split = (t.R + BK - 1) / BK * BK;
-  gemm_tile_kernel<O, AR, BR, BM, BN, BK, STAGES, WGS><<<t.tiles_i * t.tiles_j, kThreads, 0, st>>>(t);
-  RESIST_CHECK_LAUNCH("linear");
+// the product of a call, its operands laid out first where they have to be, what was split joined after
+template <typename O, int NP, bool AR, bool BR>
+int product(const Layout &l, const void *a, const void *b, long long I, int J, long long R, const Epilogue &e, float *db, void *work, const char *name,
+            double flops, double bytes, hipStream_t st) {
+  char *ws = static_cast<char *>(work);
+  float *sums = db ? reinterpret_cast<float *>(ws + l.sums_at) : nullptr;
+  if (l.a.moved || l.b.moved) {
+    LayOutArgs args{};
+    int n = 0;
+    double moved = 0.;
+    auto add = [&](const Operand &o, const void *from, float *to_sums) {
+      if (!o.moved) return;
+      LayOut &m = args.m[n++];
+      m = LayOut{from, reinterpret_cast<__bf16 *>(ws + o.at), reinterpret_cast<unsigned *>(ws + o.flags_at), to_sums, o.rows, o.ld, o.plane, o.n, (int)o.to_ld, 0, 0};
+      m.blocks_n = (o.n + 63) / 64;
+      m.blocks = (int)((o.rows + 63) / 64 * m.blocks_n);
+      moved += (NP == 3 ? 10. : 4.) * o.rows * o.n;
+    };
+    add(l.a, a, NP == 3 ? sums : nullptr);
+    add(l.b, b, nullptr);
+    prof::Scope sc("linear_lay_out", 0., moved, st);
+    lay_out_kernel<NP><<<args.m[0].blocks + args.m[1].blocks, kThreads, 0, st>>>(args);
+    RESIST_CHECK_LAUNCH("linear_lay_out");
+  }
+  TileArgs t{};
+  t.a = reinterpret_cast<const __bf16 *>(l.a.moved ? ws + l.a.at : static_cast<const char *>(a));
+  t.b = reinterpret_cast<const __bf16 *>(l.b.moved ? ws + l.b.at : static_cast<const char *>(b));
+  t.lda = l.a.to_ld; t.ldb = l.b.to_ld; t.I = I; t.J = J; t.R = R;
+  t.splits = l.plan.splits; t.per_split = l.plan.per_split; t.part = reinterpret_cast<float *>(ws + l.part_at);
+  t.sums = NP == 1 ? sums : nullptr;
+  if (NP == 3) {
+    t.plane_a = l.a.plane; t.plane_b = l.b.plane;
+    t.flags_a = reinterpret_cast<const unsigned *>(ws + l.a.flags_at); t.flags_b = reinterpret_cast<const unsigned *>(ws + l.b.flags_at);
+    t.a32 = static_cast<const float *>(a); t.b32 = static_cast<const float *>(b); t.lda32 = l.a.ld; t.ldb32 = l.b.ld;
+  }
+  t.e = e;
+  {
+    prof::Scope sc(name, flops, bytes, st);
+    if constexpr (NP == 1) {
+      if (l.plan.size == 0) RESIST_TRY((launch_tiles<O, AR, BR, 1, 256, 256, 64, 2, 1>(t, st)));
+      else if (l.plan.size == 1) RESIST_TRY((launch_tiles<O, AR, BR, 1, 128, 128, 64, 2, 2>(t, st)));
+      else RESIST_TRY((launch_tiles<O, AR, BR, 1, 64, 64, 64, 4, 2>(t, st)));
+    } else {
+      if (l.plan.size == 0) RESIST_TRY((launch_tiles<O, AR, BR, 3, 256, 128, 32, 2, 1>(t, st)));
+      else if (l.plan.size == 1) RESIST_TRY((launch_tiles<O, AR, BR, 3, 128, 128, 32, 3, 1>(t, st)));
+      else RESIST_TRY((launch_tiles<O, AR, BR, 3, 64, 64, 32, 3, 2>(t, st)));
+    }
+  }
+  if (t.splits == 1 && !db) return RESIST_OK;
+  JoinArgs j{};
+  j.part = t.part; j.splits = t.splits; j.I = I; j.J = J; j.e = e;
+  j.sums = sums; j.db = db; j.sum_parts = l.sum_parts; j.sum_n = (int)I; j.sum_wgs = db ? (int)((I + 63) / 64) : 0;
+  const long long wgs = j.sum_wgs + (t.splits > 1 ? (I * ((J + 7) / 8) + kThreads - 1) / kThreads : 0);
+  if (wgs > 0x7fffffffLL) return set_error(RESIST_ESHAPE, "linear: too many outputs");
+  prof::Scope sc("linear_join", 0., t.splits > 1 ? (double)t.splits * I * J * 4 : 0., st);
+  gemm_join_kernel<O><<<(unsigned)wgs, kThreads, 0, st>>>(j);
+  RESIST_CHECK_LAUNCH("linear_join");
   return RESIST_OK;
 }
-#ifndef RESIST_CFG
-#define RESIST_CFG 256, 256, 64, 2, 1
-#endif
-template <typename O, bool AR, bool BR> int gemm_tiles(TileArgs &t, hipStream_t st) {
-  return gemm_tiles_of<O, AR, BR, RESIST_CFG>(t, st);
-}
+
+double flops_of(const LinearShape &s) { return 2. * s.M * s.N * s.K; }
+double bytes_of(const LinearShape &s, int dt, double outs) { return ((double)s.M * s.K + (double)s.N * s.K + (double)s.M * s.N) * esize(dt) + outs; }
 
 }  // namespace
 
-int64_t linear_workspace(const LinearShape &s, int dt, int op) { (void)s; (void)dt; (void)op; return 0; }
-
-int linear_fwd(const LinearShape &s, int dt, const void *x, const void *w, const LinearEpilogue &le, void *y, void *, hipStream_t st) {
-  if (s.M == 0) return RESIST_OK;
-  GemmArgs g{};
-  g.a = x; g.ai = s.ldx; g.ar = 1; g.I = s.M;
-  g.b = w; g.bj = s.K; g.br = 1; g.J = s.N; g.R = s.K;
-  g.e.out = y; g.e.ldo = s.ldy; g.e.bias = le.bias; g.e.z_out = le.z; g.e.ldz = le.ldz; g.e.res = le.residual; g.e.ldr = le.ldr;
-  g.e.act = le.act; g.e.d = make_dropout(le.drop); g.e.words = (s.N + 1) / 2;
-  if (dt == DT_BF16 && s.K % 8 == 0 && s.ldx % 8 == 0) {
-    TileArgs t{};
-    t.a = (const __bf16 *)x; t.b = (const __bf16 *)w; t.lda = s.ldx; t.ldb = s.K; t.I = s.M; t.J = s.N; t.R = s.K; t.e = g.e;
-    return gemm_tiles<__bf16, true, true>(t, st);
-  }
-  prof::Scope sc("linear_fwd", 2. * s.M * s.N * s.K, ((double)s.M * s.K + (double)s.N * s.K + (double)s.M * s.N) * esize(dt), st);
-  return dt == DT_F32 ? gemm_any<float, float, true, true>(g, st) : gemm_any<__bf16, __bf16, true, true>(g, st);
+int64_t linear_workspace(const LinearShape &s, int dt, int op) {
+  if (s.M == 0 || (op == 0 && s.M <= kFewRows)) return 0;
+  return layout_of(s, dt, op).bytes;
 }
 
-int linear_dgrad(const LinearShape &s, int dt, const void *dz, const void *w, const LinearThrough &lt, void *dx, void *, hipStream_t st) {
+int linear_fwd(const LinearShape &s, int dt, const void *x, const void *w, const LinearEpilogue &le, void *y, void *work, hipStream_t st) {
   if (s.M == 0) return RESIST_OK;
-  GemmArgs g{};
-  g.a = dz; g.ai = s.ldy; g.ar = 1; g.I = s.M;
-  g.b = w; g.bj = 1; g.br = s.K; g.J = s.K; g.R = s.N;
-  g.e.out = dx; g.e.ldo = s.ldx; g.e.z_in = lt.act == RESIST_ACT_NONE ? nullptr : lt.z; g.e.ldz = lt.ldz; g.e.act = lt.act;
-  g.e.d = make_dropout(lt.drop); g.e.words = (s.K + 1) / 2;
-  if (dt == DT_BF16 && s.N % 8 == 0 && s.K % 8 == 0 && s.ldy % 8 == 0) {
-    TileArgs t{};
-    t.a = (const __bf16 *)dz; t.b = (const __bf16 *)w; t.lda = s.ldy; t.ldb = s.K; t.I = s.M; t.J = s.K; t.R = s.N; t.e = g.e;
-    return gemm_tiles<__bf16, true, false>(t, st);
+  Epilogue e{};
+  e.out = y; e.ldo = s.ldy; e.bias = le.bias; e.z_out = le.z; e.ldz = le.ldz; e.res = le.residual; e.ldr = le.ldr; e.act = le.act;
+  e.d = make_dropout(le.drop); e.words = (s.N + 1) / 2;
+  const double bytes = bytes_of(s, dt, (double)s.M * s.N * esize(dt) * ((le.z != nullptr) + (le.residual != nullptr)));
+  if (s.M <= kFewRows) {
+    const FewArgs f{x, w, s.ldx, (int)s.M, s.K, s.N, e};
+    prof::Scope sc("linear_few_rows", flops_of(s), bytes, st);
+    if (dt == DT_F32) few_rows_kernel<float><<<(s.N + 15) / 16, 512, 0, st>>>(f);
+    else few_rows_kernel<__bf16><<<(s.N + 15) / 16, 512, 0, st>>>(f);
+    RESIST_CHECK_LAUNCH("linear_few_rows");
+    return RESIST_OK;
   }
-  prof::Scope sc("linear_dgrad", 2. * s.M * s.N * s.K, ((double)s.M * s.K + (double)s.N * s.K + (double)s.M * s.N) * esize(dt), st);
-  return dt == DT_F32 ? gemm_any<float, float, true, false>(g, st) : gemm_any<__bf16, __bf16, true, false>(g, st);
+  const Layout l = layout_of(s, dt, 0);
+  return dt == DT_F32 ? product<float, 3, true, true>(l, x, w, s.M, s.N, s.K, e, nullptr, work, "linear_fwd", flops_of(s), bytes, st)
+                      : product<__bf16, 1, true, true>(l, x, w, s.M, s.N, s.K, e, nullptr, work, "linear_fwd", flops_of(s), bytes, st);
 }
 
-int linear_wgrad(const LinearShape &s, int dt, const void *dz, const void *x, float *dw, float *db, void *, hipStream_t st) {
-  GemmArgs g{};
-  g.a = dz; g.ai = 1; g.ar = s.ldy; g.I = s.N;
-  g.b = x; g.bj = 1; g.br = s.ldx; g.J = s.K; g.R = s.M;
-  g.e.out = dw; g.e.ldo = s.K;
-  if (dw && dt == DT_BF16 && s.ldx % 8 == 0 && s.ldy % 8 == 0) {
-    TileArgs t{};
-    t.a = (const __bf16 *)dz; t.b = (const __bf16 *)x; t.lda = s.ldy; t.ldb = s.ldx; t.I = s.N; t.J = s.K; t.R = s.M; t.e = g.e;
-    RESIST_TRY((gemm_tiles<float, false, false>(t, st)));
-  } else if (dw) {
-    prof::Scope sc("linear_wgrad", 2. * s.M * s.N * s.K, ((double)s.M * s.K + (double)s.M * s.N) * esize(dt) + 4. * s.N * s.K, st);
-    RESIST_TRY((dt == DT_F32 ? gemm_any<float, float, false, false>(g, st) : gemm_any<__bf16, float, false, false>(g, st)));
+int linear_dgrad(const LinearShape &s, int dt, const void *dz, const void *w, const LinearThrough &lt, void *dx, void *work, hipStream_t st) {
+  if (s.M == 0) return RESIST_OK;
+  Epilogue e{};
+  e.out = dx; e.ldo = s.ldx; e.z_in = lt.act == RESIST_ACT_NONE ? nullptr : lt.z; e.ldz = lt.ldz; e.act = lt.act;
+  e.d = make_dropout(lt.drop); e.words = (s.K + 1) / 2;
+  const Layout l = layout_of(s, dt, 1);
+  const double bytes = bytes_of(s, dt, e.z_in ? (double)s.M * s.K * esize(dt) : 0.);
+  return dt == DT_F32 ? product<float, 3, true, false>(l, dz, w, s.M, s.K, s.N, e, nullptr, work, "linear_dgrad", flops_of(s), bytes, st)
+                      : product<__bf16, 1, true, false>(l, dz, w, s.M, s.K, s.N, e, nullptr, work, "linear_dgrad", flops_of(s), bytes, st);
+}
+
+int linear_wgrad(const LinearShape &s, int dt, const void *dz, const void *x, float *dw, float *db, void *work, hipStream_t st) {
+  if (!dw) {
+    if (!db) return RESIST_OK;
+    prof::Scope sc("linear_bias", 0., (double)s.M * s.N * esize(dt), st);
+    if (dt == DT_F32) col_sum_kernel<float><<<(s.N + 63) / 64, kThreads, 0, st>>>(static_cast<const float *>(dz), s.M, s.N, s.ldy, db);
+    else col_sum_kernel<__bf16><<<(s.N + 63) / 64, kThreads, 0, st>>>(static_cast<const __bf16 *>(dz), s.M, s.N, s.ldy, db);
+    RESIST_CHECK_LAUNCH("linear_bias");
+    return RESIST_OK;
   }
-  if (!db) return RESIST_OK;
-  prof::Scope sc("linear_bias", 0., (double)s.M * s.N * esize(dt), st);
-  if (dt == DT_F32) col_sum_kernel<float><<<(s.N + 63) / 64, kThreads, 0, st>>>(static_cast<const float *>(dz), s.M, s.N, s.ldy, db);
-  else col_sum_kernel<__bf16><<<(s.N + 63) / 64, kThreads, 0, st>>>(static_cast<const __bf16 *>(dz), s.M, s.N, s.ldy, db);
-  RESIST_CHECK_LAUNCH("linear_bias");
-  return RESIST_OK;
+  Epilogue e{};
+  e.out = dw; e.ldo = s.K;
+  const Layout l = layout_of(s, dt, 2);
+  const double bytes = ((double)s.M * s.K + (double)s.M * s.N) * esize(dt) + 4. * s.N * s.K;
+  return dt == DT_F32 ? product<float, 3, false, false>(l, dz, x, s.N, s.K, s.M, e, db, work, "linear_wgrad", flops_of(s), bytes, st)
+                      : product<float, 1, false, false>(l, dz, x, s.N, s.K, s.M, e, db, work, "linear_wgrad", flops_of(s), bytes, st);
 }
 
 }  // namespace resist
