@@ -12,6 +12,7 @@ namespace resist {
 namespace {
 
 constexpr int kThreads = 256;
+constexpr int threads_of(int tpr) { return tpr > kThreads ? tpr : kThreads; }   // of a workgroup whose rows take tpr threads each
 constexpr int kHeldCols = 8192;   // widest row that the threads of a workgroup hold in registers
 
 struct LnArgs {
@@ -25,27 +26,58 @@ struct LnArgs {
   float eps;
 };
 
-// the sum over the TPR threads of a row; `red`: [waves of the workgroup] when a row is a workgroup's
-template <int TPR> __device__ inline float row_sum(float v, float *red) {
-#pragma unroll
-  for (int d = 1; d < (TPR < 64 ? TPR : 64); d <<= 1) v += __shfl_xor(v, d, 64);
-  if constexpr (TPR > 64) {
-    constexpr int W = TPR / 64;
-    __syncthreads();
-    if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = v;
-    __syncthreads();
-    v = 0.f;
-#pragma unroll
-    for (int w = 0; w < W; ++w) v += red[w];
+// The sum over LANES neighbouring lanes (16, 32 or 64), in every one of them, on the vector unit alone (a shuffle goes through LDS): of lanes one and
+// two apart, of the mirrored halves of eight and sixteen, of rows of sixteen, of halves of the wave.
+template <int LANES> __device__ inline float lanes_sum(float v) {
+  auto moved = [&](auto ctrl) { return __builtin_bit_cast(float, __builtin_amdgcn_mov_dpp(__builtin_bit_cast(int, v), decltype(ctrl)::value, 0xf, 0xf, true)); };
+  v += moved(std::integral_constant<int, 0xb1>{});    // quad_perm 1 0 3 2
+  v += moved(std::integral_constant<int, 0x4e>{});    // quad_perm 2 3 0 1
+  v += moved(std::integral_constant<int, 0x141>{});   // row_half_mirror
+  v += moved(std::integral_constant<int, 0x140>{});   // row_mirror
+  // v in both operands swaps every second row (half) of one with the row before it of the other: one gets each pair's first row twice, the other
+  // its second.
+  if constexpr (LANES > 16) {
+    const unsigned x = __builtin_bit_cast(unsigned, v);
+    const auto p = __builtin_amdgcn_permlane16_swap(x, x, false, false);
+    const unsigned first = p[0], second = p[1];   // (a bit cast of a vector's element itself takes the first one)
+    v = __builtin_bit_cast(float, first) + __builtin_bit_cast(float, second);
   }
+  if constexpr (LANES > 32) {
+    const unsigned x = __builtin_bit_cast(unsigned, v);
+    const auto p = __builtin_amdgcn_permlane32_swap(x, x, false, false);
+    const unsigned first = p[0], second = p[1];   // (a bit cast of a vector's element itself takes the first one)
+    v = __builtin_bit_cast(float, first) + __builtin_bit_cast(float, second);
+  }
+  return v;
+}
+// The sums over the TPR threads of a row.  red: [2][waves of the workgroup], where a row is a workgroup's; `turn` alternates from call to call, so
+// that one barrier is enough: who writes a turn's words has met everyone since they were read.
+template <int TPR> __device__ inline void row_sums(float &a, float &b, float2 (*red)[8], int turn) {
+  a = lanes_sum<(TPR < 64 ? TPR : 64)>(a);
+  b = lanes_sum<(TPR < 64 ? TPR : 64)>(b);
+  if constexpr (TPR > 64) {
+    if ((threadIdx.x & 63) == 0) red[turn][threadIdx.x >> 6] = float2{a, b};
+    __syncthreads();
+    a = b = 0.f;
+#pragma unroll
+    for (int w = 0; w < TPR / 64; ++w) {
+      const float2 t = red[turn][w];
+      a += t.x;
+      b += t.y;
+    }
+  }
+}
+template <int TPR> __device__ inline float row_sum(float v, float2 (*red)[8], int turn) {
+  float none = 0.f;
+  row_sums<TPR>(v, none, red, turn);
   return v;
 }
 
 // TPR threads a row, NV vectors of eight each
 template <typename T, int TPR, int NV>
-__global__ __launch_bounds__(kThreads) void ln_fwd_kernel(LnArgs a) {
-  __shared__ float red[kThreads / 64];
-  constexpr int RPW = kThreads / TPR;
+__global__ __launch_bounds__(threads_of(TPR)) void ln_fwd_kernel(LnArgs a) {
+  __shared__ float2 red[2][8];
+  constexpr int RPW = threads_of(TPR) / TPR;
   const int t = threadIdx.x % TPR;
   const long long row = (long long)blockIdx.x * RPW + threadIdx.x / TPR;
   const bool live = row < a.M;
@@ -59,7 +91,7 @@ __global__ __launch_bounds__(kThreads) void ln_fwd_kernel(LnArgs a) {
   }
 #pragma unroll
   for (int i = 0; i < NV; ++i) s += ((v[i][0] + v[i][1]) + (v[i][2] + v[i][3])) + ((v[i][4] + v[i][5]) + (v[i][6] + v[i][7]));
-  const float mu = row_sum<TPR>(s, red) / (float)a.N;
+  const float mu = row_sum<TPR>(s, red, 0) / (float)a.N;
   float q = 0.f;
 #pragma unroll
   for (int i = 0; i < NV; ++i) {
@@ -71,7 +103,7 @@ __global__ __launch_bounds__(kThreads) void ln_fwd_kernel(LnArgs a) {
       q += d * d;
     }
   }
-  const float r = 1.f / sqrtf(row_sum<TPR>(q, red) / (float)a.N + a.eps);
+  const float r = 1.f / sqrtf(row_sum<TPR>(q, red, 1) / (float)a.N + a.eps);
   if (!live) return;
   T *y = static_cast<T *>(a.out) + row * a.ldo;
 #pragma unroll
@@ -99,7 +131,7 @@ __global__ __launch_bounds__(kThreads) void ln_fwd_kernel(LnArgs a) {
 // rows that do not fit: a workgroup reads each three times (the second and third from L2)
 template <typename T>
 __global__ __launch_bounds__(kThreads) void ln_fwd_long_kernel(LnArgs a) {
-  __shared__ float red[kThreads / 64];
+  __shared__ float2 red[2][8];
   const long long row = blockIdx.x;
   const T *x = static_cast<const T *>(a.x) + row * a.ldx;
   T *y = static_cast<T *>(a.out) + row * a.ldo;
@@ -108,7 +140,7 @@ __global__ __launch_bounds__(kThreads) void ln_fwd_long_kernel(LnArgs a) {
     row_load(x + c, a.N - c, v);
     s += ((v[0] + v[1]) + (v[2] + v[3])) + ((v[4] + v[5]) + (v[6] + v[7]));
   }
-  const float mu = row_sum<kThreads>(s, red) / (float)a.N;
+  const float mu = row_sum<kThreads>(s, red, 0) / (float)a.N;
   float q = 0.f;
   for (int c = threadIdx.x * 8; c < a.N; c += kThreads * 8) {
     row_load(x + c, a.N - c, v);
@@ -120,7 +152,7 @@ __global__ __launch_bounds__(kThreads) void ln_fwd_long_kernel(LnArgs a) {
     }
     q += p;
   }
-  const float r = 1.f / sqrtf(row_sum<kThreads>(q, red) / (float)a.N + a.eps);
+  const float r = 1.f / sqrtf(row_sum<kThreads>(q, red, 1) / (float)a.N + a.eps);
   for (int c = threadIdx.x * 8; c < a.N; c += kThreads * 8) {
     float g[8], b[8];
     row_load(x + c, a.N - c, v);
@@ -144,9 +176,9 @@ __global__ __launch_bounds__(kThreads) void ln_fwd_long_kernel(LnArgs a) {
 // A workgroup takes rows blockIdx.x, + gridDim.x, ... (a row per TPR threads): its threads keep their columns, so dy xhat and dy are summed
 // over its rows in registers.  The threads of other rows add theirs through LDS at the end.
 template <typename T, int TPR, int NV>
-__global__ __launch_bounds__(kThreads) void ln_bwd_kernel(LnArgs a) {
-  constexpr int RPW = kThreads / TPR;
-  __shared__ float red[kThreads / 64];
+__global__ __launch_bounds__(threads_of(TPR)) void ln_bwd_kernel(LnArgs a) {
+  constexpr int RPW = threads_of(TPR) / TPR;
+  __shared__ float2 red[2][8];
   const int t = threadIdx.x % TPR, sub = threadIdx.x / TPR;
   float sg[NV][8], sb[NV][8];
 #pragma unroll
@@ -154,48 +186,71 @@ __global__ __launch_bounds__(kThreads) void ln_bwd_kernel(LnArgs a) {
 #pragma unroll
     for (int e = 0; e < 8; ++e) sg[i][e] = sb[i][e] = 0.f;
   const long long step = (long long)gridDim.x * RPW;
+  // a row's operands are asked for while the one before it is worked on
+  Raw8<T> rx[NV], rdy[NV], rad[NV];
+  float mu, r;
+  auto ask = [&](long long row) {
+    const bool live = row < a.M;
+    const long long rr = live ? row : 0;
+    const T *x = static_cast<const T *>(a.x) + rr * a.ldx, *dy = static_cast<const T *>(a.dy) + rr * a.lddy, *ad = static_cast<const T *>(a.addend) + rr * a.lda;
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+      const int c = (t + i * TPR) * 8, left = live ? a.N - c : 0;
+      raw_load(x + c, left, rx[i]);
+      raw_load(dy + c, left, rdy[i]);
+      if (a.addend) raw_load(ad + c, left, rad[i]);
+    }
+    mu = a.mean[rr];
+    r = a.rstd[rr];
+  };
+  float w[NV][8];
+#pragma unroll
+  for (int i = 0; i < NV; ++i) {
+    const int c = (t + i * TPR) * 8;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) w[i][e] = 1.f;
+    if (a.gamma) row_load(a.gamma + c, a.N - c, w[i]);
+  }
+  int turn = 0;
+  ask((long long)blockIdx.x * RPW + sub);
   for (long long row0 = (long long)blockIdx.x * RPW; row0 < a.M; row0 += step) {
     const long long row = row0 + sub;
     const bool live = row < a.M;
-    const long long rr = live ? row : 0;
-    const T *x = static_cast<const T *>(a.x) + rr * a.ldx, *dy = static_cast<const T *>(a.dy) + rr * a.lddy;
-    const float mu = a.mean[rr], r = a.rstd[rr];
+    const float rs = r;
     float g[NV][8], h[NV][8], s1 = 0.f, s2 = 0.f;
+    Raw8<T> add[NV];
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
       const int c = (t + i * TPR) * 8, left = live ? a.N - c : 0;
-      row_load(x + c, left, h[i]);
-      row_load(dy + c, left, g[i]);
-    }
-#pragma unroll
-    for (int i = 0; i < NV; ++i) {
-      const int c = (t + i * TPR) * 8, left = live ? a.N - c : 0;
-      float w[8];
-      if (a.gamma) row_load(a.gamma + c, left, w);
+      widen(rx[i], h[i]);
+      widen(rdy[i], g[i]);
+      add[i] = rad[i];
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
-        h[i][e] = e < left ? (h[i][e] - mu) * r : 0.f;
+        h[i][e] = e < left ? (h[i][e] - mu) * rs : 0.f;
         sg[i][e] += g[i][e] * h[i][e];
         sb[i][e] += g[i][e];
-        if (a.gamma) g[i][e] *= w[e];
+        g[i][e] *= w[i][e];
         s1 += g[i][e];
         s2 += g[i][e] * h[i][e];
       }
     }
-    s1 = row_sum<TPR>(s1, red) / (float)a.N;
-    s2 = row_sum<TPR>(s2, red) / (float)a.N;
+    ask(row + step);
+    row_sums<TPR>(s1, s2, red, turn);
+    turn ^= 1;
+    s1 /= (float)a.N;
+    s2 /= (float)a.N;
     if (!live) continue;
     T *dx = static_cast<T *>(a.out) + row * a.ldo;
-    const T *ad = static_cast<const T *>(a.addend) + row * a.lda;
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
       const int c = (t + i * TPR) * 8, left = a.N - c;
       if (left <= 0) break;
       float o[8];
-      if (a.addend) row_load(ad + c, left, o);
+      if (a.addend) widen(add[i], o);
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
-        const float d = r * (g[i][e] - s1 - h[i][e] * s2);
+        const float d = rs * (g[i][e] - s1 - h[i][e] * s2);
         o[e] = a.addend ? o[e] + d : d;
       }
       row_store(dx + c, left, o);
@@ -236,7 +291,7 @@ __global__ __launch_bounds__(kThreads) void ln_bwd_kernel(LnArgs a) {
 // rows that do not fit: the sums of the rows first ...
 template <typename T>
 __global__ __launch_bounds__(kThreads) void ln_bwd_rows_kernel(LnArgs a, float *sums) {
-  __shared__ float red[kThreads / 64];
+  __shared__ float2 red[2][8];
   const long long row = blockIdx.x;
   const T *x = static_cast<const T *>(a.x) + row * a.ldx, *dy = static_cast<const T *>(a.dy) + row * a.lddy;
   const float mu = a.mean[row], r = a.rstd[row];
@@ -254,8 +309,9 @@ __global__ __launch_bounds__(kThreads) void ln_bwd_rows_kernel(LnArgs a, float *
     }
     s1 += p1; s2 += p2;
   }
-  s1 = row_sum<kThreads>(s1, red) / (float)a.N;
-  s2 = row_sum<kThreads>(s2, red) / (float)a.N;
+  row_sums<kThreads>(s1, s2, red, 0);
+  s1 /= (float)a.N;
+  s2 /= (float)a.N;
   if (threadIdx.x == 0) { sums[2 * row] = s1; sums[2 * row + 1] = s2; }
 }
 // ... then, 2048 columns of a range of rows to a workgroup, the gradients
@@ -287,13 +343,20 @@ __global__ __launch_bounds__(kThreads) void ln_bwd_cols_kernel(LnArgs a, const f
   row_store(p + a.N + c, left, sb);
 }
 
-// columns [2][N] of `parts` parts, in float64: 64 columns to a workgroup, 16 ranges of parts, joined in order
+// Columns [2][N] of `parts` parts, in float64: 64 columns to a workgroup, 16 ranges of parts (eight of each on their way at once), joined in order.
 __global__ __launch_bounds__(1024) void ln_params_kernel(const float *part, int parts, int N, float *dgamma, float *dbeta) {
   __shared__ double red[16][64];
   const int c = blockIdx.x * 64 + (threadIdx.x & 63), k = threadIdx.x >> 6;
   double s = 0.;
-  if (c < 2 * N)
-    for (int p = k; p < parts; p += 16) s += (double)part[(size_t)p * 2 * N + c];
+  if (c < 2 * N) {
+    for (int p0 = k; p0 < parts; p0 += 128) {
+      float v[8];
+#pragma unroll
+      for (int i = 0; i < 8; ++i) v[i] = p0 + i * 16 < parts ? part[(size_t)(p0 + i * 16) * 2 * N + c] : 0.f;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) s += (double)v[i];
+    }
+  }
   red[k][threadIdx.x & 63] = s;
   __syncthreads();
   if (k != 0 || c >= 2 * N) return;
@@ -303,31 +366,46 @@ __global__ __launch_bounds__(1024) void ln_params_kernel(const float *part, int 
   if (out) out[c < N ? c : c - N] = (float)s;
 }
 
-// threads a row and vectors a thread
+// Threads a row and vectors a thread: as few threads as hold a row in one or two vectors each, so that a wave takes several short rows at once.
 struct Held { int tpr, nv; };
 Held held_shape(int N) {
-  Held h;
-  h.tpr = N > 1024 ? 256 : 64;
-  h.nv = 1;
-  while (h.tpr * h.nv * 8 < N) h.nv *= 2;
-  return h;
+  if (N <= 128) return Held{16, 1};
+  if (N <= 256) return Held{32, 1};
+  if (N <= 512) return Held{64, 1};
+  if (N <= 1024) return Held{64, 2};
+  if (N <= 2048) return Held{256, 1};
+  return N <= 4096 ? Held{256, 2} : Held{512, 2};
 }
+// Workgroups of the backward pass, each of which leaves a part of the columns' sums: two a CU (one where it is 512 threads) where there are rows enough for
+// two or more apiece (four where a part is long); with up to 64 rows (or groups of them) a row each, which is quicker than a second turn.
+// us, M x N, with 1 | 2 | 4 rows a turn:  777x513 fp32 12.0 | 11.7 | 13.6   2000x300 bf16 16.2 | 12.8 | 13.4   300x2000 bf16 13.9 | 11.2 | 11.7
+//   1000x4096 fp32 27.1 | 26.8 | 22.1   64x1024 fp32 7.8 | 8.7 | 10.8       16384x4096 bf16, 256 | 512 | 1024 workgroups 142 | 109 | 132
 int bwd_parts(int64_t M, int N) {
-  const int64_t rpw = N > kHeldCols ? 1 : kThreads / held_shape(N).tpr;
-  return (int)std::max<int64_t>(1, std::min<int64_t>(512, (M + rpw - 1) / rpw));
+  const Held h = held_shape(N);
+  const int64_t rpw = N > kHeldCols ? 1 : threads_of(h.tpr) / h.tpr, turns = (M + rpw - 1) / rpw, each = N > 2048 ? 4 : 2;
+  const int64_t most = h.tpr == 512 && N <= kHeldCols ? 256 : 512;
+  return (int)std::max<int64_t>(1, std::min<int64_t>(most, std::max<int64_t>(std::min<int64_t>(64, turns), (turns + each - 1) / each)));
 }
+// call(kernel<T, TPR, NV>, threads) for the shape of N
+#define LN_HELD(kernel, T, N, call)                                               \
+  do {                                                                            \
+    const Held h = held_shape(N);                                                 \
+    if (h.tpr == 16) call((kernel<T, 16, 1>), 16);                                \
+    else if (h.tpr == 32) call((kernel<T, 32, 1>), 32);                           \
+    else if (h.tpr == 64 && h.nv == 1) call((kernel<T, 64, 1>), 64);              \
+    else if (h.tpr == 64) call((kernel<T, 64, 2>), 64);                           \
+    else if (h.tpr == 256 && h.nv == 1) call((kernel<T, 256, 1>), 256);           \
+    else if (h.tpr == 256) call((kernel<T, 256, 2>), 256);                        \
+    else call((kernel<T, 512, 2>), 512);                                          \
+  } while (0)
 
 template <typename T> int fwd(const LnArgs &a, hipStream_t st) {
   if (a.N > kHeldCols) {
     ln_fwd_long_kernel<T><<<dim3((unsigned)a.M), kThreads, 0, st>>>(a);
   } else {
-    const Held h = held_shape(a.N);
-    const dim3 grid((unsigned)((a.M + kThreads / h.tpr - 1) / (kThreads / h.tpr)));
-    if (h.tpr == 64 && h.nv == 1) ln_fwd_kernel<T, 64, 1><<<grid, kThreads, 0, st>>>(a);
-    else if (h.tpr == 64) ln_fwd_kernel<T, 64, 2><<<grid, kThreads, 0, st>>>(a);
-    else if (h.nv == 1) ln_fwd_kernel<T, 256, 1><<<grid, kThreads, 0, st>>>(a);
-    else if (h.nv == 2) ln_fwd_kernel<T, 256, 2><<<grid, kThreads, 0, st>>>(a);
-    else ln_fwd_kernel<T, 256, 4><<<grid, kThreads, 0, st>>>(a);
+#define FWD(k, tpr) k<<<(unsigned)((a.M + threads_of(tpr) / tpr - 1) / (threads_of(tpr) / tpr)), threads_of(tpr), 0, st>>>(a)
+    LN_HELD(ln_fwd_kernel, T, a.N, FWD);
+#undef FWD
   }
   RESIST_CHECK_LAUNCH("layernorm_fwd");
   return RESIST_OK;
@@ -337,12 +415,9 @@ template <typename T> int bwd(const LnArgs &a, int parts, float *sums, hipStream
     ln_bwd_rows_kernel<T><<<dim3((unsigned)a.M), kThreads, 0, st>>>(a, sums);
     ln_bwd_cols_kernel<T><<<dim3(parts, (a.N + kThreads * 8 - 1) / (kThreads * 8)), kThreads, 0, st>>>(a, sums);
   } else {
-    const Held h = held_shape(a.N);
-    if (h.tpr == 64 && h.nv == 1) ln_bwd_kernel<T, 64, 1><<<parts, kThreads, 0, st>>>(a);
-    else if (h.tpr == 64) ln_bwd_kernel<T, 64, 2><<<parts, kThreads, 0, st>>>(a);
-    else if (h.nv == 1) ln_bwd_kernel<T, 256, 1><<<parts, kThreads, 0, st>>>(a);
-    else if (h.nv == 2) ln_bwd_kernel<T, 256, 2><<<parts, kThreads, 0, st>>>(a);
-    else ln_bwd_kernel<T, 256, 4><<<parts, kThreads, 0, st>>>(a);
+#define BWD(k, tpr) k<<<parts, threads_of(tpr), 0, st>>>(a)
+    LN_HELD(ln_bwd_kernel, T, a.N, BWD);
+#undef BWD
   }
   RESIST_CHECK_LAUNCH("layernorm_bwd");
   return RESIST_OK;

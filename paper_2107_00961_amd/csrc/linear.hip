@@ -166,14 +166,15 @@ struct TileArgs {
   Epilogue e;
 };
 
-// eight outputs of a row.  bias: of their columns; side: what the epilogue reads beside them, z (data gradient) or the residual (forward)
+// Eight outputs of a row, at `out`; z goes to `z_out` (optional), `word` is the number of the dropout's first word.  bias: of their columns; side: what
+// the epilogue reads beside them, z (data gradient) or the residual (forward)
 template <typename O>
-__device__ inline void finish8(const Epilogue &e, long long i, int j, int left, float (&v)[8], const float (&bias)[8], const Raw8<O> &side, u64 base) {
+__device__ inline void finish8(const Epilogue &e, O *out, O *z_out, u64 word, int left, float (&v)[8], const float (&bias)[8], const Raw8<O> &side, u64 base) {
 #pragma unroll
   for (int k = 0; k < 8; ++k) v[k] += bias[k];
-  if (e.z_out) row_store(static_cast<O *>(e.z_out) + i * e.ldz + j, left, v);
+  if (e.z_out) row_store(z_out, left, v);
   if (!e.z_in) activate(v, e.act);
-  if (e.d.rng) dropout8(base, (u64)i * (unsigned)e.words + (unsigned)(j >> 1), e.d.thr, e.d.scale, v);
+  if (e.d.rng) dropout8(base, word, e.d.thr, e.d.scale, v);
   if (e.z_in || e.res) {
     float s[8];
     widen(side, s);
@@ -184,7 +185,7 @@ __device__ inline void finish8(const Epilogue &e, long long i, int j, int left, 
       for (int k = 0; k < 8; ++k) v[k] += s[k];
     }
   }
-  row_store(static_cast<O *>(e.out) + i * e.ldo + j, left, v);
+  row_store(out, left, v);
 }
 template <typename O> __device__ inline const O *side_of(const Epilogue &e, long long &ld) {
   ld = e.z_in ? e.ldz : e.ldr;
@@ -486,39 +487,79 @@ __global__ __launch_bounds__(kThreads, WGS) void gemm_tile_kernel(TileArgs g) {
     v0 = *reinterpret_cast<const f32x4 *>(p);
     v1 = *reinterpret_cast<const f32x4 *>(p + 16);
   };
-  long long ld_side;
-  const O *side = side_of<O>(g.e, ld_side);
-  const bool has_side = side != nullptr && whole;
-  Raw8<O> ahead[kAhead] = {};
-  auto ask = [&](int pass, Raw8<O> &r) {
-    const long long row = row0 + pass * RPP;
-    if (pass < TM * PASSES && row < g.I && left > 0) raw_load(side + row * ld_side + j, left, r);
-  };
-  float bias[8] = {};
-  if (whole) bias_of(g.e, j, left, bias);
-  if (has_side) {
-#pragma unroll
-    for (int p = 0; p < kAhead; ++p) ask(p, ahead[p]);
-  }
-  put(std::integral_constant<int, 0>{});
-  get(0);
-#pragma unroll 1
-  for (int pass = 0; pass < TM * PASSES; ++pass) {
-    if (TM > 1 && pass == 0) put(std::integral_constant<int, TM - 1 < 1 ? TM - 1 : 1>{});
-    if (TM > 2 && pass == PASSES) put(std::integral_constant<int, TM - 1 < 2 ? TM - 1 : 2>{});
-    if (TM > 3 && pass == 2 * PASSES) put(std::integral_constant<int, TM - 1 < 3 ? TM - 1 : 3>{});
-    float v[8] = {v0[0], v0[1], v0[2], v0[3], v1[0], v1[1], v1[2], v1[3]};
-    get(pass + 1 < TM * PASSES ? pass + 1 : pass);
-    const Raw8<O> now = ahead[0];
+  if (j0 + BN > g.J || (whole && (g.e.act != RESIST_ACT_NONE || g.e.d.rng || g.e.z_out || g.e.res || g.e.z_in))) {
+    long long ld_side;
+    const O *side = side_of<O>(g.e, ld_side);
+    const bool has_side = side != nullptr && whole;
+    side += row0 * ld_side + j;
+    O *out = static_cast<O *>(g.e.out) + row0 * g.e.ldo + j, *z_out = static_cast<O *>(g.e.z_out) + row0 * g.e.ldz + j;
+    float *part = g.part + ((long long)split * g.I + row0) * g.J + j;
+    u64 word = (u64)row0 * (unsigned)g.e.words + (unsigned)(j >> 1);
+    int rows = (int)min(g.I - row0, (long long)BM);   // of the operand from this lane's first on
+    if (left <= 0) rows = 0;
+    Raw8<O> ahead[kAhead] = {};
+    auto ask = [&](int pass, Raw8<O> &r) {
+      if (pass * RPP < rows && pass < TM * PASSES) raw_load(side, left, r);
+      side += RPP * ld_side;
+    };
+    float bias[8] = {};
+    if (whole) bias_of(g.e, j, left, bias);
     if (has_side) {
 #pragma unroll
-      for (int p = 0; p + 1 < kAhead; ++p) ahead[p] = ahead[p + 1];
-      ask(pass + kAhead, ahead[kAhead - 1]);
+      for (int p = 0; p < kAhead; ++p) ask(p, ahead[p]);
     }
-    const long long row = row0 + pass * RPP;
-    if (row >= g.I || left <= 0) continue;
-    if (whole) finish8<O>(g.e, row, j, left, v, bias, now, base);
-    else row_store(g.part + ((long long)split * g.I + row) * g.J + j, left, v);
+    put(std::integral_constant<int, 0>{});
+    get(0);
+#pragma unroll 1
+    for (int pass = 0; pass < TM * PASSES; ++pass) {
+      if (TM > 1 && pass == 0) put(std::integral_constant<int, TM - 1 < 1 ? TM - 1 : 1>{});
+      if (TM > 2 && pass == PASSES) put(std::integral_constant<int, TM - 1 < 2 ? TM - 1 : 2>{});
+      if (TM > 3 && pass == 2 * PASSES) put(std::integral_constant<int, TM - 1 < 3 ? TM - 1 : 3>{});
+      float v[8] = {v0[0], v0[1], v0[2], v0[3], v1[0], v1[1], v1[2], v1[3]};
+      get(pass + 1 < TM * PASSES ? pass + 1 : pass);
+      const Raw8<O> now = ahead[0];
+      if (has_side) {
+#pragma unroll
+        for (int p = 0; p + 1 < kAhead; ++p) ahead[p] = ahead[p + 1];
+        ask(pass + kAhead, ahead[kAhead - 1]);
+      }
+      if (pass * RPP < rows) {
+        if (whole) finish8<O>(g.e, out, z_out, word, left, v, bias, now, base);
+        else row_store(part, left, v);
+      }
+      part += (long long)RPP * g.J;
+      out += RPP * g.e.ldo;
+      z_out += RPP * g.e.ldz;
+      word += RPP * (unsigned)g.e.words;
+    }
+  } else {
+    // Sums on their own, or with a bias, in whole vectors: a pass is little more than its store, unrolled
+    float bias[8] = {};
+    if (whole) bias_of(g.e, j, 8, bias);
+    const int rows = (int)min(g.I - row0, (long long)BM);
+    auto all = [&](auto *out, long long ld) {
+      auto chunk = [&](auto kc) {
+        constexpr int k = decltype(kc)::value;
+        if constexpr (k < TM) {
+          put(kc);
+#pragma unroll
+          for (int p = 0; p < PASSES; ++p) {
+            get(k * PASSES + p);
+            float v[8] = {v0[0], v0[1], v0[2], v0[3], v1[0], v1[1], v1[2], v1[3]};
+#pragma unroll
+            for (int e = 0; e < 8; ++e) v[e] += bias[e];
+            if ((k * PASSES + p) * RPP < rows) Row<std::remove_pointer_t<decltype(out)>>::store(out, v);
+            out += RPP * ld;
+          }
+        }
+      };
+      chunk(std::integral_constant<int, 0>{});
+      chunk(std::integral_constant<int, 1>{});
+      chunk(std::integral_constant<int, 2>{});
+      chunk(std::integral_constant<int, 3>{});
+    };
+    if (whole) all(static_cast<O *>(g.e.out) + row0 * g.e.ldo + j, g.e.ldo);
+    else all(g.part + ((long long)split * g.I + row0) * g.J + j, (long long)g.J);
   }
 }
 
@@ -563,7 +604,8 @@ __global__ __launch_bounds__(kThreads) void gemm_join_kernel(JoinArgs a) {
 #pragma unroll
     for (int k = 0; k < 8; ++k) v[k] += w[k];
   }
-  finish8<O>(a.e, row, j, left, v, bias, now, a.e.d.rng ? dropout_base(a.e.d.rng) : 0);
+  finish8<O>(a.e, static_cast<O *>(a.e.out) + row * a.e.ldo + j, static_cast<O *>(a.e.z_out) + row * a.e.ldz + j, (u64)row * (unsigned)a.e.words + (unsigned)(j >> 1), left, v, bias, now,
+             a.e.d.rng ? dropout_base(a.e.d.rng) : 0);
 }
 
 // ---- few rows -------------------------------------------------------------------------------------------------------
@@ -644,29 +686,44 @@ __global__ __launch_bounds__(kThreads) void col_sum_kernel(const T *dz, long lon
 // ---- plans ----------------------------------------------------------------------------------------------------------
 constexpr int kFewRows = 16;
 
+// Which tiles, and how many ranges of the reduction (`splits`): the least time by a model of the kernels, us, with what was measured alone on the chip:
+// a launch, then rounds of as many workgroups as fit (one or two a CU), each its start and epilogue and `step` per 64 of the reduction
+// (`low` with a quarter of that many, `full` with all: the clock gives way under the products); a split reduction writes
+// its parts and reads them back in a launch of its own.  Either side of the choice, us measured, bf16 forward unless said
+// (M x K x N: 256x256 | 128x128 | 64x64):
+//   8192x8192x2048  212 | 261 | -       4096x2048x2048  54 | 38 | 61     512x4096x4096  89 | 49 | 30      64x512x512  16 | 8.3 | 5.6
+//   128x4096x512, 64x64: 1 split 21.4, 2 14.8, 4 11.2, 8 10.7            128x512x4096, 64x64: 1 split 5.7, 2 9.4, 4 11.5
+//   fp32 2048x1024x4096 (256x128 | 128x128 | 64x64)  100 | 108 | 146     fp32 2000x1024x1024  74 | 49 (2 splits 42) | 47
+struct TileCost { int bm, bn, fit; double start, low, full; };
+constexpr TileCost kTiles[2][3] = {{{256, 256, 256, 7.0, 1.15, 1.58}, {128, 128, 512, 2.6, 0.58, 1.03}, {64, 64, 512, 1.4, 0.28, 0.42}},
+                                   {{256, 128, 256, 5.0, 3.2, 5.0}, {128, 128, 256, 3.0, 1.75, 2.6}, {64, 64, 512, 1.5, 0.81, 2.0}}};
+constexpr double kLaunch = 2.0, kJoin = 3.0, kBytesPerUs = 3.5e6;
 struct Plan {
   int size;                  // of the tiles: 0 the largest ... 2 the smallest
   int bm, bn, splits;
   long long per_split;
 };
-#ifndef RESIST_PLAN
-#define RESIST_PLAN -1, 0
-#endif
-constexpr int kForce[2] = {RESIST_PLAN};
 Plan plan_tiles(int np, long long I, long long J, long long R) {
-  static const int bm[2][3] = {{256, 128, 64}, {256, 128, 64}}, bn[2][3] = {{256, 128, 64}, {128, 128, 64}};
-  const int f = np == 3;
-  Plan p{};
-  p.size = I * J >= 256LL * 256 * 128 ? 0 : I * J >= 128 * 128 * 64 ? 1 : 2;
-  if (kForce[0] >= 0) p.size = kForce[0];
-  p.bm = bm[f][p.size]; p.bn = bn[f][p.size];
-  p.splits = 1;
-  if (kForce[1] > 0) p.splits = kForce[1];
   const long long steps = (R + 63) / 64;
-  p.splits = (int)std::min<long long>(p.splits, steps);
-  p.per_split = (steps + p.splits - 1) / p.splits * 64;
-  p.splits = (int)((R + p.per_split - 1) / p.per_split);
-  return p;
+  Plan best{};
+  double least = 0.;
+  for (int size = 0; size < 3; ++size) {
+    const TileCost &c = kTiles[np == 3][size];
+    const long long tiles = ((I + c.bm - 1) / c.bm) * ((J + c.bn - 1) / c.bn);
+    for (const int want : {1, 2, 3, 4, 6, 8, 12, 16, 24, 32}) {
+      if (want > 1 && (want > steps / 4 || tiles * want > 2 * c.fit)) break;
+      const long long per = (steps + want - 1) / want, splits = (steps + per - 1) / per, wgs = tiles * splits;
+      const long long rounds = wgs / c.fit, rest = wgs - rounds * c.fit;
+      double t = kLaunch + rounds * (c.start + per * c.full);
+      if (rest > 0) t += c.start + per * (rest * 4 <= c.fit ? c.low : rest * 2 <= c.fit ? 0.5 * (c.low + c.full) : c.full);
+      if (splits > 1) t += kJoin + 8. * splits * I * J / kBytesPerUs;
+      if (best.splits == 0 || t < least) {
+        least = t;
+        best = Plan{size, c.bm, c.bn, (int)splits, per * 64};
+      }
+    }
+  }
+  return best;
 }
 
 // An operand of a call: `rows` rows of n elements; whether it has to be laid out, and where.
