@@ -480,41 +480,39 @@ def stem_conv2d_wgrad(dy, x, w_shape, stride, pad, stream=None):
 # contiguous or not 16-byte aligned at the start is copied first.  Results are new tensors, allocated for the stream the call runs on:
 # the current one, or `stream`.
 ACTIVATIONS = {"none": 0, "relu": 1, "gelu": 2, "gelu_tanh": 3, "silu": 4}
-_DTYPES = {}   # torch dtype -> code, filled by the first call (torch is imported where it is needed)
-_here = None
+torch = None     # and what the calls below need of it, from the first of them on: most take less time than torch.cuda.current_stream()
+_DTYPES = {}     # torch dtype -> code
+_INT64 = ()
+_F32 = _raw_stream = _device = None
 
 
-def _make_here():
-    """_here(t, stream): the current stream (hipStream_t) where the call can run as things stand, on t's device; None where it has to be
-    moved there first (_there).  Most of these calls take less time than torch.cuda.current_stream() alone."""
+def _start():
+    global torch, _F32, _INT64, _raw_stream, _device
     import torch
+    _F32, _INT64 = torch.float32, (torch.int64, torch.uint64)
     _DTYPES.update({torch.float32: 0, torch.bfloat16: 1})
-    device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
-    raw = getattr(torch._C, "_cuda_getCurrentRawStream", lambda i: torch.cuda.current_stream(i).cuda_stream)
-
-    def here(t, stream):
-        if not t.is_cuda:
-            raise ResistError("device tensors only: there is no CPU path")
-        i = t.get_device()
-        if stream is not None:
-            if stream.device_index != i:
-                raise ResistError(f"a stream of device {stream.device_index} for tensors on {t.device}")
-            return None
-        return raw(i) if device() == i else None
-    return here
+    _device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
+    _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", lambda i: torch.cuda.current_stream(i).cuda_stream)
 
 
 def _on(t, stream):
-    global _here
-    if _here is None:
-        _here = _make_here()
-    return _here(t, stream)
+    """The current stream (hipStream_t) where the call can run as things stand, on t's device; None where it has to be moved there
+    first (_there)."""
+    if torch is None:
+        _start()
+    if not t.is_cuda:
+        raise ResistError("device tensors only: there is no CPU path")
+    i = t.get_device()
+    if stream is not None:
+        if stream.device_index != i:
+            raise ResistError(f"a stream of device {stream.device_index} for tensors on {t.device}")
+        return None
+    return _raw_stream(i) if _device() == i else None
 
 
 def _there(call, stream, *args):
     """The call with its first tensor's device as the current one, on `stream` (None: that device's current stream).  Memory of its inputs that is
     given back meanwhile waits for a stream that is not their own."""
-    import torch
     with torch.cuda.device(args[0].device):
         if stream is None:
             return call(*args)
@@ -537,7 +535,7 @@ def _matrix(t, what, like=None, shape=None):
     """t as rows the library takes; checked against the call's first tensor."""
     if t.dim() != 2:
         raise ResistError(f"{what}: a matrix [rows, N] is needed, got {tuple(t.shape)}")
-    if like is not None and (t.dtype != like.dtype or t.device != like.device):
+    if like is not None and (t.dtype != like.dtype or t.get_device() != like.get_device()):
         raise ResistError(f"{what}: {t.dtype} on {t.device} beside {like.dtype} on {like.device}")
     m, n = t.shape
     if shape is not None and (m, n) != shape:
@@ -547,8 +545,7 @@ def _matrix(t, what, like=None, shape=None):
     if t.is_contiguous():
         return t if t.data_ptr() % 16 == 0 else t.clone()
     if t.stride(1) != 1 and n > 1 or t.stride(0) < n and m > 1 or t.data_ptr() % 16:
-        import torch
-        t = t.clone(memory_format=torch.contiguous_format)
+        t = t.contiguous()
     return t
 
 
@@ -561,7 +558,9 @@ def _vector(t, what, n, like):
     """A parameter vector [n] float32, or None -> itself, contiguous and aligned."""
     if t is None:
         return None
-    if _DTYPES.get(t.dtype) != 0 or t.device != like.device or t.dim() != 1 or t.shape[0] != n:
+    if torch is None:
+        _start()
+    if t.dtype is not _F32 or t.get_device() != like.get_device() or t.dim() != 1 or t.numel() != n:
         raise ResistError(f"{what}: float32 [{n}] on {like.device} is needed, got {t.dtype} {tuple(t.shape)} on {t.device}")
     return t if t.is_contiguous() and t.data_ptr() % 16 == 0 else t.clone()
 
@@ -572,8 +571,9 @@ def _rng_ptr(rng, p, like):
         if p:
             raise ResistError("rng: needed where p is not 0")
         return None
-    import torch
-    if rng.dtype not in (torch.int64, torch.uint64) or rng.device != like.device or tuple(rng.shape) != (2,) or not rng.is_contiguous():
+    if torch is None:
+        _start()
+    if rng.dtype not in _INT64 or rng.get_device() != like.get_device() or rng.dim() != 1 or rng.numel() != 2 or not rng.is_contiguous():
         raise ResistError(f"rng: two contiguous 64-bit integers on {like.device} are needed")
     return rng.data_ptr()
 
@@ -594,13 +594,12 @@ def layernorm_forward(x, gamma=None, beta=None, eps=1e-5, stream=None):
     st = _on(x, stream)
     if st is None:
         return _there(layernorm_forward, stream, x, gamma, beta, eps)
-    import torch
     dt = _dtype_of(x)
     x = _matrix(x, "x")
     M, N = x.shape
     gamma, beta = _vector(gamma, "gamma", N, x), _vector(beta, "beta", N, x)
     y = x.new_empty((M, N))
-    mean, rstd = x.new_empty(M, dtype=torch.float32), x.new_empty(M, dtype=torch.float32)
+    mean, rstd = x.new_empty(M, dtype=_F32), x.new_empty(M, dtype=_F32)
     _check(lib().resist_layernorm_forward(M, N, dt, x.data_ptr(), _ld(x), _opt(gamma), _opt(beta), eps, y.data_ptr(), 0, mean.data_ptr(),
                                           rstd.data_ptr(), st))
     return y, mean, rstd
@@ -619,7 +618,6 @@ def layernorm_backward(dy, x, gamma, mean, rstd, addend=None, stream=None):
     st = _on(dy, stream)
     if st is None:
         return _there(layernorm_backward, stream, dy, x, gamma, mean, rstd, addend)
-    import torch
     dt = _dtype_of(dy)
     dy = _matrix(dy, "dy")
     M, N = dy.shape
@@ -630,7 +628,7 @@ def layernorm_backward(dy, x, gamma, mean, rstd, addend=None, stream=None):
         raise ResistError("mean and rstd: those of layernorm_forward are needed")
     mean, rstd = _vector(mean, "mean", M, dy), _vector(rstd, "rstd", M, dy)
     dx = dy.new_empty((M, N))
-    dgamma, dbeta = dy.new_empty(N, dtype=torch.float32), dy.new_empty(N, dtype=torch.float32)
+    dgamma, dbeta = dy.new_empty(N, dtype=_F32), dy.new_empty(N, dtype=_F32)
     n = _layernorm_ws(M, N)
     ws = dy.new_empty(n, dtype=torch.uint8)
     _check(lib().resist_layernorm_backward(M, N, dt, dy.data_ptr(), _ld(dy), x.data_ptr(), _ld(x), _opt(gamma), mean.data_ptr(), rstd.data_ptr(),
@@ -681,7 +679,6 @@ def _linear_ws(like, op, *shape):
     n = _linear_ws_bytes(*shape, op)
     if not n:
         return None, 0
-    import torch
     return like.new_empty(n, dtype=torch.uint8), n
 
 
@@ -742,7 +739,6 @@ def linear_wgrad(dz, x, stream=None):
     st = _on(dz, stream)
     if st is None:
         return _there(linear_wgrad, stream, dz, x)
-    import torch
     dt = _dtype_of(dz)
     dz = _matrix(dz, "dz")
     M, N = dz.shape
@@ -750,7 +746,7 @@ def linear_wgrad(dz, x, stream=None):
     if x.shape[0] != M:
         raise ResistError(f"x: {x.shape[0]} rows beside {M} of dz")
     K = x.shape[1]
-    dw, db = dz.new_empty((N, K), dtype=torch.float32), dz.new_empty(N, dtype=torch.float32)
+    dw, db = dz.new_empty((N, K), dtype=_F32), dz.new_empty(N, dtype=_F32)
     ldx, ldy = _ld(x), _ld(dz)
     ws, n = _linear_ws(dz, 2, M, K, N, ldx, ldy, dt)
     _check(lib().resist_linear_wgrad(_LinearShape(M, K, N, ldx, ldy, dt), dz.data_ptr(), x.data_ptr(), dw.data_ptr(), db.data_ptr(), _opt(ws), n, st))
