@@ -129,8 +129,8 @@ __global__ __launch_bounds__(kThreads) void lay_out_kernel(LayOutArgs a) {
 // in fragments to the matrix cores.  Four waves, a quarter of the BM x BN tile each: the larger a wave's share, the fewer times a
 // staged element is read from LDS (256x256: 1024 clocks of reading and 512 of arriving for 2048 of products).
 // Layout in LDS.  Lane order leaves no room for padding, so what keeps rows off each other's banks is which 16-byte piece a lane asks for:
-//   reduction contiguous (R): a row is an index i, BK values of r: piece c of row i lies at c ^ f(i), f = i & 7 (BK 64, 128 bytes a row),
-//     (i >> 1) & 3 (BK 32, two rows to 128 bytes): eight consecutive rows' pieces c fill 128 bytes;
+//   reduction contiguous (R): a row is an index i, BK values of r: piece c of row i lies at c ^ f(i), f = (i >> 1) & 7 (BK 64, two rows to 256
+//     bytes), (i >> 2) & 3 (BK 32, four rows): sixteen consecutive rows' pieces c fill the 256 bytes of the 64 banks;
 //   other index contiguous: a row is an r, BM values of i: piece c of row r lies at c ^ 4 (r & 3) (64 values, two rows to 256 bytes:
 //     c ^ 2 (r & 2)): the four rows of a transpose read, 64 bytes each, fill 256 bytes.
 // Bounds: an operand's descriptor starts at the tile and ends with the operand (rows past it, and steps past it, come as zeros); its
@@ -141,7 +141,7 @@ template <bool R, int B, int BK> struct Stage {
   static constexpr int kBytes = B * BK * 2, kLoads = kBytes / 4096;   // of a plane; a wave's instructions
   static constexpr int kRow = R ? BK * 2 : B * 2, kPieces = kRow / 16, kRows = 1024 / kRow;   // rows an instruction
   __device__ static inline int swizzle(int row) {
-    if (R) return BK == 64 ? row & 7 : (row >> 1) & 3;
+    if (R) return BK == 64 ? (row >> 1) & 7 : (row >> 2) & 3;
     return kPieces == 8 ? (row & 2) << 1 : (row & 3) << 2;
   }
   // row and piece of the tile that lane `l` of wave `w` asks for with instruction p
@@ -206,6 +206,8 @@ template <int N> __device__ inline void wait_and_meet() {   // at most N of this
   asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(N) : "memory");
 }
 
+__device__ inline void meet() { asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory"); }   // all reads done
+
 // the tile's place: `group` rows of tiles are walked column by column, an XCD's workgroups one after the other
 __device__ inline void tile_of(int bid, int tiles_i, int tiles_j, int group, int &ti, int &tj) {
   const int per = group * tiles_j, g = bid / per, rest = bid - g * per;
@@ -260,6 +262,11 @@ __global__ __launch_bounds__(kThreads, WGS) void gemm_tile_kernel(TileArgs g) {
   constexpr int kLoadsA = NP * SA::kLoads, kLoads = kLoadsA + NP * SB::kLoads, kA = NP * SA::kBytes, kStage = kA + NP * SB::kBytes;
   constexpr int kPitch = WTN * 4 + 16, kOut = 4 * 2 * 32 * kPitch;
   static_assert(STAGES >= 2, "stages");
+  // Two stages only: a step's fragments are read in its first half, and what is staged next goes where they came from in the second half and the
+  // following step's first: transfers have two products of depth 16 or more to arrive in, and a stage less does.  (Fragments are
+  // read a product ahead else, and a stage is free a step later.  Waiting for transfers took 11 % of the 256x256 tile's time then.)
+  constexpr bool EARLY = STAGES == 2 && BK == 64 && NP == 1;
+  constexpr int SETS = EARLY ? NK : 2;
   static_assert(TM <= 4, "tile");
   __shared__ __attribute__((aligned(1024))) char lds[STAGES * kStage > kOut ? STAGES * kStage : kOut];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), wm = wave >> 1, wn = wave & 1;
@@ -331,7 +338,7 @@ __global__ __launch_bounds__(kThreads, WGS) void gemm_tile_kernel(TileArgs g) {
       ob[j] = fr * SB::kRow + (((c >> 3) ^ SB::swizzle(fr)) << 4) + (c & 7) * 2;
     }
   }
-  bf16x8 fa[2][NP][TM], fb[2][NP][TN];
+  bf16x8 fa[SETS][NP][TM], fb[SETS][NP][TN];
   constexpr int kFrags = NP * (TM + TN);
   auto fetch = [&](int n, int set, int stage, int k) {   // fragment n, plane by plane from the smallest part on, of a plane A's first, B's, the rest of A's
     const int p = NP - 1 - n / (TM + TN), m = n % (TM + TN);
@@ -355,8 +362,8 @@ __global__ __launch_bounds__(kThreads, WGS) void gemm_tile_kernel(TileArgs g) {
 #pragma unroll
       for (int e = 0; e < 16; ++e) acc[i][j][e] = 0.f;
 
-  // A step of the reduction asks for the tile STAGES steps ahead, whose place in LDS is free once all waves have met at the end of
-  // the step before it: an NK-th of its transfers then, an NK-th with each of the first NK-1 of its NK products of depth 16.
+  // A step of the reduction asks for the tile STAGES steps ahead, whose place in LDS is free once all waves have met: an NK-th of its transfers with
+  // each of NK products of depth 16, from the last of the step before on (early: from the third).
   constexpr int kEach = kLoads / NK;
   static_assert(kLoads % NK == 0 && (STAGES - 2) * kLoads + kEach < 64, "transfers");
 #pragma unroll
@@ -365,9 +372,10 @@ __global__ __launch_bounds__(kThreads, WGS) void gemm_tile_kernel(TileArgs g) {
     for (int p = 0; p < kLoads; ++p) request(p, s);
     advance();
   }
+  constexpr int kFirst = EARLY ? 2 * kEach : kEach;
 #pragma unroll
-  for (int p = 0; p < kEach; ++p) request(p, STAGES - 1);
-  wait_and_meet<(STAGES - 2) * kLoads + kEach>();
+  for (int p = 0; p < kFirst; ++p) request(p, STAGES - 1);
+  wait_and_meet<(STAGES - 2) * kLoads + kFirst>();
 #pragma unroll
   for (int n = 0; n < kFrags; ++n) fetch(n, 0, 0, 0);
   __builtin_amdgcn_sched_barrier(0);
@@ -377,23 +385,38 @@ __global__ __launch_bounds__(kThreads, WGS) void gemm_tile_kernel(TileArgs g) {
   float sums[TM] = {};
   int sums_at = kSums && g.sums ? tj : 0x7fffffff;
   auto step = [&](auto kc, int next, bool take) {
-    constexpr int k = decltype(kc)::value, PAIRS = NP == 3 ? 6 : 1, MF = PAIRS * TM * TN, MD = MF > 1 ? MF * 3 / 4 : 1, MH = MF > 1 ? MF / 2 : 1;
+    constexpr int k = decltype(kc)::value, PAIRS = NP == 3 ? 6 : 1, MF = PAIRS * TM * TN, MD = MF > 1 ? MF * 3 / 4 : 1, MH = EARLY || MF == 1 ? MF : MF / 2;
     constexpr bool last = k + 1 == NK;
-    if constexpr (last) {
+    constexpr int set = EARLY ? k : k & 1;
+    if constexpr (EARLY && k == 2) {
       advance();
-      wait_and_meet<(STAGES - 2) * kLoads>();
+      meet();                                   // everyone has read this stage
     }
+    if constexpr (last) {
+      if constexpr (!EARLY) advance();
+      wait_and_meet<EARLY ? kEach : (STAGES - 2) * kLoads>();   // the next stage is there
+    }
+    // fragments read beside these products: the next one's; early, of the 3 kFrags that are left of this step half with each of its first two
+    // products, and with the last one the next step's first
+    constexpr int d0 = EARLY && k < 2 ? k * 3 * kFrags / 2 : 0, d1 = EARLY ? (k < 2 ? (k + 1) * 3 * kFrags / 2 : last ? kFrags : 0) : kFrags, DS = d1 - d0;
     int ds = 0, vm = 0;
 #pragma unroll
     for (int m = 0; m < MF; ++m) {   // a product, then what goes on beside it, in this order
       const int pair = m / (TM * TN), i = m / TN % TM, j = m % TN;
       const int pa_ = NP == 1 ? 0 : pair == 0 ? 2 : pair == 1 ? 0 : pair == 2 ? 1 : pair == 3 ? 1 : 0;   // parts l h', h l', m m', m h', h m', h h'
       const int pb_ = NP == 1 ? 0 : pair == 0 ? 0 : pair == 1 ? 2 : pair == 2 ? 1 : pair == 3 ? 0 : pair == 4 ? 1 : 0;
-      acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fb[k & 1][pb_][j], fa[k & 1][pa_][i], acc[i][j], 0, 0, 0);
+      acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fb[set][pb_][j], fa[set][pa_][i], acc[i][j], 0, 0, 0);
 #pragma unroll
-      for (; ds < (m + 1 < MD ? (m + 1) * kFrags / MD : kFrags); ++ds) fetch(ds, (k + 1) & 1, last ? next : stage, last ? 0 : k + 1);
+      for (; ds < (m + 1 < MD ? (m + 1) * DS / MD : DS); ++ds) {
+        if constexpr (EARLY && !last) fetch((d0 + ds) % kFrags, 1 + (d0 + ds) / kFrags, stage, 1 + (d0 + ds) / kFrags);
+        else if constexpr (EARLY) fetch(ds, 0, next, 0);
+        else fetch(ds, (k + 1) & 1, last ? next : stage, last ? 0 : k + 1);
+      }
 #pragma unroll
-      for (; vm < (m + 1 < MH ? (m + 1) * kEach / MH : kEach); ++vm) request(last ? vm : (k + 1) * kEach + vm, last ? stage : refill);
+      for (; vm < (m + 1 < MH ? (m + 1) * kEach / MH : kEach); ++vm) {
+        if constexpr (EARLY) request(((k + 2) % NK) * kEach + vm, k < 2 ? next : stage);
+        else request(last ? vm : (k + 1) * kEach + vm, last ? stage : refill);
+      }
       __builtin_amdgcn_sched_barrier(0);
     }
     if constexpr (kSums) {
@@ -401,7 +424,7 @@ __global__ __launch_bounds__(kThreads, WGS) void gemm_tile_kernel(TileArgs g) {
 #pragma unroll
         for (int i = 0; i < TM; ++i)
 #pragma unroll
-          for (int e = 0; e < 8; ++e) sums[i] += (float)fa[k & 1][0][i][e];
+          for (int e = 0; e < 8; ++e) sums[i] += (float)fa[set][0][i][e];
       }
     }
   };
