@@ -260,7 +260,7 @@ __global__ __launch_bounds__(kThreads, WGS) void gemm_tile_kernel(TileArgs g) {
   using SB = Stage<BR, BN, BK>;
   constexpr int WTM = BM / 2, WTN = BN / 2, TM = WTM / 32, TN = WTN / 32, NK = BK / 16;
   constexpr int kLoadsA = NP * SA::kLoads, kLoads = kLoadsA + NP * SB::kLoads, kA = NP * SA::kBytes, kStage = kA + NP * SB::kBytes;
-  constexpr int kPitch = WTN * 4 + 16, kOut = 4 * 2 * 32 * kPitch;
+  constexpr int kPitch = WTN * 4 + 16, kSide = AR ? 32 * WTN * (int)sizeof(O) : 0, kOut = 4 * (32 * kPitch + kSide);
   static_assert(STAGES >= 2, "stages");
   // Two stages only: a step's fragments are read in its first half, and what is staged next goes where they came from in the second half and the
   // following step's first: transfers have two products of depth 16 or more to arrive in, and a stage less does.  (Fragments are
@@ -442,9 +442,9 @@ __global__ __launch_bounds__(kThreads, WGS) void gemm_tile_kernel(TileArgs g) {
     stage = next;
   }
 
-  // ---- out: 32 rows of a wave's share at a time through LDS, so that memory sees whole rows of it.  One wave a SIMD has nothing to hide a
-  // wait behind but its own next rows: they are on their way from LDS, what the epilogue reads beside them for the next kAhead passes from
-  // memory, while a pass is worked on.  One copy of the code (it is long, and the instruction cache is shared).
+  // ---- out: 32 rows of a wave's share at a time through LDS, so that memory sees whole rows of it.  What the epilogue reads beside them is asked for
+  // up front, all of it (the fragments' registers are free), and passes through LDS, too, where a loop can index it: one wave a SIMD has nothing
+  // else to hide a wait behind, and a copy of the code for each pass would not fit the instruction cache.
   asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");   // the steps past the end have arrived too
   if constexpr (kSums) {
     if (g.sums) {
@@ -486,94 +486,114 @@ __global__ __launch_bounds__(kThreads, WGS) void gemm_tile_kernel(TileArgs g) {
       return;
     }
   }
-  char *const mine = lds + wave * 2 * 32 * kPitch;
   const bool whole = g.splits == 1;
   const u64 base = g.e.d.rng && whole ? dropout_base(g.e.d.rng) : 0;
-  constexpr int LPR = WTN / 8, RPP = 64 / LPR, PASSES = 32 / RPP, kAhead = sizeof(O) == 2 ? 8 : 4;   // lanes a row, rows a pass, passes of 32 rows
+  constexpr int LPR = WTN / 8, RPP = 64 / LPR, PASSES = 32 / RPP;   // lanes a row, rows a pass, passes of 32 rows
+  static_assert(!AR || sizeof(Raw8<O>) * PASSES * 64 <= (size_t)kSide, "LDS");
+  char *const mine = lds + wave * (32 * kPitch + kSide);
+  Raw8<O> *const mine_side = reinterpret_cast<Raw8<O> *>(mine + 32 * kPitch) + lane;   // a lane's own
   const int c = (lane % LPR) * 8, j = j0 + wn * WTN + c, left = g.J - j;
   const long long row0 = i0 + wm * WTM + lane / LPR;
+  const int rows = left <= 0 ? 0 : (int)min(g.I - row0, (long long)BM);   // of the operand from this lane's first on
   auto put = [&](auto kc) {
     constexpr int k = decltype(kc)::value;
 #pragma unroll
     for (int n = 0; n < TN; ++n)
 #pragma unroll
       for (int q = 0; q < 4; ++q)
-        *reinterpret_cast<f32x4 *>(mine + (k & 1) * 32 * kPitch + lr * kPitch + (n * 32 + q * 8 + lg * 4) * 4) =
+        *reinterpret_cast<f32x4 *>(mine + lr * kPitch + (n * 32 + q * 8 + lg * 4) * 4) =
             f32x4{acc[k][n][q * 4], acc[k][n][q * 4 + 1], acc[k][n][q * 4 + 2], acc[k][n][q * 4 + 3]};
     asm volatile("" ::"n"(k));   // left alone, the compiler makes one of the calls, with an index, and keeps the sums in memory for it
+  };
+  auto meet_lanes = [&]() {   // LDS takes a wave's accesses in order: it is the compiler that has to
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
     __builtin_amdgcn_wave_barrier();
   };
   f32x4 v0, v1;
-  auto get = [&](int pass) {   // rows of pass `pass` of all
-    const char *p = mine + (pass / PASSES & 1) * 32 * kPitch + (pass % PASSES * RPP + lane / LPR) * kPitch + c * 4;
-    v0 = *reinterpret_cast<const f32x4 *>(p);
-    v1 = *reinterpret_cast<const f32x4 *>(p + 16);
+  Raw8<O> vs;
+  auto get = [&](int p) {   // pass p of the 32 rows
+    const char *at = mine + (p * RPP + lane / LPR) * kPitch + c * 4;
+    v0 = *reinterpret_cast<const f32x4 *>(at);
+    v1 = *reinterpret_cast<const f32x4 *>(at + 16);
   };
   if (j0 + BN > g.J || (whole && (g.e.act != RESIST_ACT_NONE || g.e.d.rng || g.e.z_out || g.e.res || g.e.z_in))) {
     long long ld_side;
     const O *side = side_of<O>(g.e, ld_side);
-    const bool has_side = side != nullptr && whole;
     side += row0 * ld_side + j;
+    constexpr bool kSided = AR;   // a weight gradient has nothing beside it
+    const bool has_side = kSided && whole && (g.e.z_in || g.e.res), early = has_side && j0 + BN <= g.J;
     O *out = static_cast<O *>(g.e.out) + row0 * g.e.ldo + j, *z_out = static_cast<O *>(g.e.z_out) + row0 * g.e.ldz + j;
     float *part = g.part + ((long long)split * g.I + row0) * g.J + j;
     u64 word = (u64)row0 * (unsigned)g.e.words + (unsigned)(j >> 1);
-    int rows = (int)min(g.I - row0, (long long)BM);   // of the operand from this lane's first on
-    if (left <= 0) rows = 0;
-    Raw8<O> ahead[kAhead] = {};
-    auto ask = [&](int pass, Raw8<O> &r) {
-      if (pass * RPP < rows && pass < TM * PASSES) raw_load(side, left, r);
-      side += RPP * ld_side;
-    };
     float bias[8] = {};
     if (whole) bias_of(g.e, j, left, bias);
-    if (has_side) {
+    Raw8<O> ahead[kSided ? TM : 1][PASSES];
+    if (kSided && early) {
 #pragma unroll
-      for (int p = 0; p < kAhead; ++p) ask(p, ahead[p]);
+      for (int k = 0; k < TM; ++k)
+#pragma unroll
+        for (int p = 0; p < PASSES; ++p) {
+          const int r = (k * PASSES + p) * RPP;
+          raw_load(side + (r < rows ? r : 0) * ld_side - (rows > 0 ? 0 : row0 * ld_side), 8, ahead[kSided ? k : 0][p]);   // of a row that is there, whichever
+        }
     }
-    put(std::integral_constant<int, 0>{});
-    get(0);
-#pragma unroll 1
-    for (int pass = 0; pass < TM * PASSES; ++pass) {
-      if (TM > 1 && pass == 0) put(std::integral_constant<int, TM - 1 < 1 ? TM - 1 : 1>{});
-      if (TM > 2 && pass == PASSES) put(std::integral_constant<int, TM - 1 < 2 ? TM - 1 : 2>{});
-      if (TM > 3 && pass == 2 * PASSES) put(std::integral_constant<int, TM - 1 < 3 ? TM - 1 : 3>{});
-      float v[8] = {v0[0], v0[1], v0[2], v0[3], v1[0], v1[1], v1[2], v1[3]};
-      get(pass + 1 < TM * PASSES ? pass + 1 : pass);
-      const Raw8<O> now = ahead[0];
-      if (has_side) {
+    auto bring = [&](auto kc) {
+      put(kc);
+      if (kSided && early) {
 #pragma unroll
-        for (int p = 0; p + 1 < kAhead; ++p) ahead[p] = ahead[p + 1];
-        ask(pass + kAhead, ahead[kAhead - 1]);
+        for (int p = 0; p < PASSES; ++p) mine_side[p * 64] = ahead[kSided ? decltype(kc)::value : 0][p];
       }
-      if (pass * RPP < rows) {
-        if (whole) finish8<O>(g.e, out, z_out, word, left, v, bias, now, base);
-        else row_store(part, left, v);
+    };
+    int at = 0;   // rows behind
+#pragma unroll 1
+    for (int k = 0; k < TM; ++k) {
+      if (k == 0) bring(std::integral_constant<int, 0>{});
+      if (TM > 1 && k == 1) bring(std::integral_constant<int, TM - 1 < 1 ? TM - 1 : 1>{});
+      if (TM > 2 && k == 2) bring(std::integral_constant<int, TM - 1 < 2 ? TM - 1 : 2>{});
+      if (TM > 3 && k == 3) bring(std::integral_constant<int, TM - 1 < 3 ? TM - 1 : 3>{});
+      meet_lanes();
+      get(0);
+#pragma unroll 1
+      for (int p = 0; p < PASSES; ++p, at += RPP) {
+        float v[8] = {v0[0], v0[1], v0[2], v0[3], v1[0], v1[1], v1[2], v1[3]};
+        get(p + 1 < PASSES ? p + 1 : p);
+        if (at < rows) {
+          if (whole) {
+            if (early) vs = mine_side[p * 64];
+            else if (has_side) raw_load(side, left, vs);
+            finish8<O>(g.e, out, z_out, word, left, v, bias, vs, base);
+          } else {
+            row_store(part, left, v);
+          }
+        }
+        side += RPP * ld_side;
+        part += (long long)RPP * g.J;
+        out += RPP * g.e.ldo;
+        z_out += RPP * g.e.ldz;
+        word += RPP * (unsigned)g.e.words;
       }
-      part += (long long)RPP * g.J;
-      out += RPP * g.e.ldo;
-      z_out += RPP * g.e.ldz;
-      word += RPP * (unsigned)g.e.words;
+      meet_lanes();
     }
   } else {
     // Sums on their own, or with a bias, in whole vectors: a pass is little more than its store, unrolled
     float bias[8] = {};
     if (whole) bias_of(g.e, j, 8, bias);
-    const int rows = (int)min(g.I - row0, (long long)BM);
     auto all = [&](auto *out, long long ld) {
       auto chunk = [&](auto kc) {
         constexpr int k = decltype(kc)::value;
         if constexpr (k < TM) {
           put(kc);
+          meet_lanes();
 #pragma unroll
           for (int p = 0; p < PASSES; ++p) {
-            get(k * PASSES + p);
+            get(p);
             float v[8] = {v0[0], v0[1], v0[2], v0[3], v1[0], v1[1], v1[2], v1[3]};
 #pragma unroll
             for (int e = 0; e < 8; ++e) v[e] += bias[e];
             if ((k * PASSES + p) * RPP < rows) Row<std::remove_pointer_t<decltype(out)>>::store(out, v);
             out += RPP * ld;
           }
+          meet_lanes();
         }
       };
       chunk(std::integral_constant<int, 0>{});
