@@ -364,15 +364,15 @@ __global__ __launch_bounds__(kThreads, WGS) void gemm_tile_kernel(TileArgs g) {
 
   // A step of the reduction asks for the tile STAGES steps ahead, whose place in LDS is free once all waves have met: an NK-th of its transfers with
   // each of NK products of depth 16, from the last of the step before on (early: from the third).
-  constexpr int kEach = kLoads / NK;
-  static_assert(kLoads % NK == 0 && (STAGES - 2) * kLoads + kEach < 64, "transfers");
+  static_assert((STAGES - 1) * kLoads < 64, "transfers");
+  auto cut = [](int k) constexpr { return k * kLoads / NK; };   // a tile's transfers cut(k) .. cut(k + 1) go together
 #pragma unroll
   for (int s = 0; s < STAGES - 1; ++s) {
 #pragma unroll
     for (int p = 0; p < kLoads; ++p) request(p, s);
     advance();
   }
-  constexpr int kFirst = EARLY ? 2 * kEach : kEach;
+  constexpr int kFirst = cut(EARLY ? 2 : 1);
 #pragma unroll
   for (int p = 0; p < kFirst; ++p) request(p, STAGES - 1);
   wait_and_meet<(STAGES - 2) * kLoads + kFirst>();
@@ -394,11 +394,12 @@ __global__ __launch_bounds__(kThreads, WGS) void gemm_tile_kernel(TileArgs g) {
     }
     if constexpr (last) {
       if constexpr (!EARLY) advance();
-      wait_and_meet<EARLY ? kEach : (STAGES - 2) * kLoads>();   // the next stage is there
+      wait_and_meet<EARLY ? cut(1) : (STAGES - 2) * kLoads>();   // the next stage is there
     }
     // fragments read beside these products: the next one's; early, of the 3 kFrags that are left of this step half with each of its first two
     // products, and with the last one the next step's first
     constexpr int d0 = EARLY && k < 2 ? k * 3 * kFrags / 2 : 0, d1 = EARLY ? (k < 2 ? (k + 1) * 3 * kFrags / 2 : last ? kFrags : 0) : kFrags, DS = d1 - d0;
+    constexpr int part = EARLY ? (k + 2) % NK : (k + 1) % NK, v0 = cut(part), VM = cut(part + 1) - v0;
     int ds = 0, vm = 0;
 #pragma unroll
     for (int m = 0; m < MF; ++m) {   // a product, then what goes on beside it, in this order
@@ -413,9 +414,9 @@ __global__ __launch_bounds__(kThreads, WGS) void gemm_tile_kernel(TileArgs g) {
         else fetch(ds, (k + 1) & 1, last ? next : stage, last ? 0 : k + 1);
       }
 #pragma unroll
-      for (; vm < (m + 1 < MH ? (m + 1) * kEach / MH : kEach); ++vm) {
-        if constexpr (EARLY) request(((k + 2) % NK) * kEach + vm, k < 2 ? next : stage);
-        else request(last ? vm : (k + 1) * kEach + vm, last ? stage : refill);
+      for (; vm < (m + 1 < MH ? (m + 1) * VM / MH : VM); ++vm) {
+        if constexpr (EARLY) request(v0 + vm, k < 2 ? next : stage);
+        else request(v0 + vm, last ? stage : refill);
       }
       __builtin_amdgcn_sched_barrier(0);
     }
@@ -652,65 +653,219 @@ __global__ __launch_bounds__(kThreads) void gemm_join_kernel(JoinArgs a) {
 }
 
 // ---- few rows -------------------------------------------------------------------------------------------------------
-// y = x w' for at most 16 rows: the time is that of reading w once.  A workgroup takes 16 rows of w, its eight waves every eighth piece of the
-// reduction; fragments of both operands come straight from memory (rows that start anywhere are fine), several in flight, and the waves'
-// sums are joined in LDS, in order.
+// The time is that of reading w once (forward, data gradient) or of writing dw once, so w comes straight from memory into fragments, from rows that
+// start anywhere, several loads in flight, and nothing is laid out.  16 of w by 16 rows, MG times, on v_mfma_f32_16x16x32_bf16 or
+// v_mfma_f32_16x16x4_f32.  A workgroup's eight waves take every eighth piece of its range of the reduction, and their sums are joined in LDS,
+// in order; where there are few workgroups the reduction is split among several (gemm_join_kernel).  Rows and columns past the last are
+// read as the last one and not stored.
 struct FewArgs {
-  const void *x, *w;
-  long long ldx;
+  const void *a, *w;        // x or dz, [M][K] or [M][N]
+  long long lda;
   int M, K, N;
+  int splits, per;          // ranges of the reduction, one per blockIdx.y; their length
+  float *part;              // [splits][M][outputs of a row]
   Epilogue e;
 };
-template <typename T>
-__global__ __launch_bounds__(512) void few_rows_kernel(FewArgs a) {
-  constexpr int V = 16 / (int)sizeof(T), STEP = 4 * V, AHEAD = 4;   // elements a lane, of the reduction a wave and load; loads in flight
+template <typename T> struct Four;   // four elements
+template <> struct Four<float> { typedef f32x4 Raw; typedef f32x4_any Any; };
+typedef u32x2 u32x2_any __attribute__((aligned(2)));
+template <> struct Four<__bf16> { typedef u32x2 Raw; typedef u32x2_any Any; };
+__device__ inline f32x4 widen4(const f32x4 &r) { return r; }
+__device__ inline f32x4 widen4(const u32x2 &r) { return f32x4{bf16_lo(r[0]), bf16_hi(r[0]), bf16_lo(r[1]), bf16_hi(r[1])}; }
+// 16 or 8 bytes of a row from element k on, with zeros from element n on
+template <typename T, typename Raw> __device__ inline Raw piece(const T *p, int k, int n) {
+  constexpr int V = (int)(sizeof(Raw) / sizeof(T));
+  Raw out = {};
+#pragma unroll
+  for (int e = 0; e < V; ++e)
+    if (k + e < n) {
+      if constexpr (sizeof(T) == 4) out[e] = p[k + e];
+      else out[e >> 1] |= (unsigned)__builtin_bit_cast(unsigned short, p[k + e]) << (e & 1 ? 16 : 0);
+    }
+  return out;
+}
+
+// y = x w': 16 rows of w to a workgroup
+template <typename T, int MG>
+__global__ __launch_bounds__(512) void few_rows_fwd_kernel(FewArgs a) {
+  constexpr int V = 16 / (int)sizeof(T), STEP = 4 * V, AHEAD = MG == 1 ? 8 : 4;   // elements a lane, of the reduction a wave and load; loads in flight
+  typedef std::conditional_t<sizeof(T) == 4, f32x4, u32x4> Piece;
+  typedef std::conditional_t<sizeof(T) == 4, f32x4_any, u32x4_any> Any;
   __shared__ float red[8][16][17];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, row = lane & 15, kk = (lane >> 4) * V;
-  const int n = blockIdx.x * 16 + row;
-  const T *w = static_cast<const T *>(a.w) + (long long)(n < a.N ? n : 0) * a.K, *x = static_cast<const T *>(a.x) + (row < a.M ? row : 0) * a.ldx;
-  f32x4 acc = {};
-  typedef std::conditional_t<sizeof(T) == 4, f32x4, u32x4> Piece;
-  auto piece = [&](const T *p, int k, bool ok, Piece &out) {   // V elements from k on, zeros past the end
-    out = Piece{};
-    if (!ok || k >= a.K) return;
-    if (k + V <= a.K) {
-      if constexpr (sizeof(T) == 4) out = *reinterpret_cast<const f32x4_any *>(p + k);
-      else out = *reinterpret_cast<const u32x4_any *>(p + k);
-    } else {
+  const int beg = blockIdx.y * a.per, end = min(a.K, beg + a.per);
+  const T *w = static_cast<const T *>(a.w) + (long long)min((int)blockIdx.x * 16 + row, a.N - 1) * a.K, *x[MG];
 #pragma unroll
-      for (int e = 0; e < V; ++e)
-        if (k + e < a.K) {
-          if constexpr (sizeof(T) == 4) out[e] = p[k + e];
-          else out[e >> 1] |= (unsigned)__builtin_bit_cast(unsigned short, p[k + e]) << (e & 1 ? 16 : 0);
-        }
-    }
-  };
-  for (int k0 = wave * STEP; k0 < a.K; k0 += 8 * STEP * AHEAD) {
-    Piece fw[AHEAD], fx[AHEAD];
+  for (int g = 0; g < MG; ++g) x[g] = static_cast<const T *>(a.a) + min(g * 16 + row, a.M - 1) * a.lda;
+  f32x4 acc[MG] = {};
+  auto multiply = [&](const Piece &fw, const Piece (&fx)[MG]) {
 #pragma unroll
-    for (int u = 0; u < AHEAD; ++u) {
-      piece(w, k0 + u * 8 * STEP + kk, n < a.N, fw[u]);
-      piece(x, k0 + u * 8 * STEP + kk, row < a.M, fx[u]);
-    }
-#pragma unroll
-    for (int u = 0; u < AHEAD; ++u) {
+    for (int g = 0; g < MG; ++g) {
       if constexpr (sizeof(T) == 4) {
 #pragma unroll
-        for (int e = 0; e < 4; ++e) acc = __builtin_amdgcn_mfma_f32_16x16x4f32(fw[u][e], fx[u][e], acc, 0, 0, 0);
+        for (int e = 0; e < 4; ++e) acc[g] = __builtin_amdgcn_mfma_f32_16x16x4f32(fw[e], fx[g][e], acc[g], 0, 0, 0);
       } else {
-        acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, fw[u]), __builtin_bit_cast(bf16x8, fx[u]), acc, 0, 0, 0);
+        acc[g] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, fw), __builtin_bit_cast(bf16x8, fx[g]), acc[g], 0, 0, 0);
       }
     }
+  };
+  int k0 = beg + wave * STEP;
+  for (; k0 + (AHEAD * 8 - 7) * STEP <= end; k0 += 8 * STEP * AHEAD) {   // all of these pieces are whole
+    Piece fw[AHEAD], fx[AHEAD][MG];
+#pragma unroll
+    for (int u = 0; u < AHEAD; ++u) {
+      fw[u] = *reinterpret_cast<const Any *>(w + k0 + u * 8 * STEP + kk);
+#pragma unroll
+      for (int g = 0; g < MG; ++g) fx[u][g] = *reinterpret_cast<const Any *>(x[g] + k0 + u * 8 * STEP + kk);
+    }
+#pragma unroll
+    for (int u = 0; u < AHEAD; ++u) multiply(fw[u], fx[u]);
   }
+#pragma unroll 1
+  for (; k0 < end; k0 += 8 * STEP) {
+    Piece fw, fx[MG];
+    if (k0 + STEP <= end) {
+      fw = *reinterpret_cast<const Any *>(w + k0 + kk);
 #pragma unroll
-  for (int e = 0; e < 4; ++e) red[wave][row][(lane >> 4) * 4 + e] = acc[e];   // lane: row `row` of x, four columns
+      for (int g = 0; g < MG; ++g) fx[g] = *reinterpret_cast<const Any *>(x[g] + k0 + kk);
+    } else {
+      fw = piece<T, Piece>(w, k0 + kk, end);
+#pragma unroll
+      for (int g = 0; g < MG; ++g) fx[g] = piece<T, Piece>(x[g], k0 + kk, end);
+    }
+    multiply(fw, fx);
+  }
+  const u64 base = a.e.d.rng && a.splits == 1 ? dropout_base(a.e.d.rng) : 0;
+#pragma unroll
+  for (int g = 0; g < MG; ++g) {
+    if (g > 0) __syncthreads();
+#pragma unroll
+    for (int e = 0; e < 4; ++e) red[wave][row][(lane >> 4) * 4 + e] = acc[g][e];   // lane: row `row` of x, four columns
+    __syncthreads();
+    const int m = g * 16 + (threadIdx.x >> 4), c = threadIdx.x & 15, j = blockIdx.x * 16 + c;
+    if (threadIdx.x < 256 && m < a.M && j < a.N) {
+      float v = red[0][m & 15][c];
+#pragma unroll
+      for (int s = 1; s < 8; ++s) v += red[s][m & 15][c];
+      if (a.splits > 1) a.part[((long long)blockIdx.y * a.M + m) * a.N + j] = v;
+      else finish<T>(a.e, m, j, v, base);
+    }
+  }
+}
+
+// dx = dz w in fp32: 64 columns of w to a workgroup.  A lane loads four columns of four rows and four elements of dz: 16 of the reduction a wave
+// and piece.  Column 4 i + c of the 64 is row i of the c-th product, so that a lane ends up with 16 columns next to each other.  (In bf16 the
+// tiles read half the bytes and are as quick.)
+template <int MG>
+__global__ __launch_bounds__(512) void few_rows_dgrad_kernel(FewArgs a) {
+  constexpr int AHEAD = MG == 4 ? 2 : 4;
+  __shared__ float red[8][16][65];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, row = lane & 15, nn = (lane >> 4) * 4;
+  const int c0 = blockIdx.x * 64 + row * 4, beg = blockIdx.y * a.per, end = min(a.N, beg + a.per);
+  const bool inside = blockIdx.x * 64 + 64 <= (unsigned)a.K;
+  const float *w = static_cast<const float *>(a.w), *z[MG];
+#pragma unroll
+  for (int g = 0; g < MG; ++g) z[g] = static_cast<const float *>(a.a) + min(g * 16 + row, a.M - 1) * a.lda;
+  f32x4 acc[MG][4] = {};
+  auto multiply = [&](const f32x4 (&fw)[4], const f32x4 (&fz)[MG]) {
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+#pragma unroll
+      for (int g = 0; g < MG; ++g)
+#pragma unroll
+        for (int c = 0; c < 4; ++c) acc[g][c] = __builtin_amdgcn_mfma_f32_16x16x4f32(fw[e][c], fz[g][e], acc[g][c], 0, 0, 0);
+  };
+  int n0 = beg + wave * 16;
+  if (inside)
+    for (; n0 + (AHEAD * 8 - 7) * 16 <= end; n0 += 8 * 16 * AHEAD) {   // all of these pieces are whole
+      f32x4 fw[AHEAD][4], fz[AHEAD][MG];
+#pragma unroll
+      for (int u = 0; u < AHEAD; ++u) {
+        const int n = n0 + u * 8 * 16 + nn;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) fw[u][e] = *reinterpret_cast<const f32x4_any *>(w + (long long)(n + e) * a.K + c0);
+#pragma unroll
+        for (int g = 0; g < MG; ++g) fz[u][g] = *reinterpret_cast<const f32x4_any *>(z[g] + n);
+      }
+#pragma unroll
+      for (int u = 0; u < AHEAD; ++u) multiply(fw[u], fz[u]);
+    }
+#pragma unroll 1
+  for (; n0 < end; n0 += 8 * 16) {
+    const int n = n0 + nn;
+    f32x4 fw[4], fz[MG];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) fw[e] = n + e < end ? piece<float, f32x4>(w + (long long)(n + e) * a.K, c0, a.K) : f32x4{};
+#pragma unroll
+    for (int g = 0; g < MG; ++g) fz[g] = piece<float, f32x4>(z[g], n, end);
+    multiply(fw, fz);
+  }
+  const u64 base = a.e.d.rng && a.splits == 1 ? dropout_base(a.e.d.rng) : 0;
+#pragma unroll
+  for (int g = 0; g < MG; ++g) {
+    if (g > 0) __syncthreads();
+#pragma unroll
+    for (int c = 0; c < 4; ++c)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) red[wave][row][(lane >> 4) * 16 + r * 4 + c] = acc[g][c][r];
+    __syncthreads();
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      const int r = (threadIdx.x >> 6) + h * 8, m = g * 16 + r, c = threadIdx.x & 63, j = blockIdx.x * 64 + c;
+      if (m >= a.M || j >= a.K) continue;
+      float v = red[0][r][c];
+#pragma unroll
+      for (int s = 1; s < 8; ++s) v += red[s][r][c];
+      if (a.splits > 1) a.part[((long long)blockIdx.y * a.M + m) * a.K + j] = v;
+      else finish<float>(a.e, m, j, v, base);
+    }
+  }
+}
+
+// dw = dz' x, db: 64 rows by 256 columns of dw to a workgroup, 16 rows to a wave, four columns of all rows of x in each lane's registers.
+template <typename T, int MR>
+__global__ __launch_bounds__(kThreads) void few_rows_wgrad_kernel(const T *dz, long long ldz, const T *x, long long ldx, int M, int N, int K, float *dw, float *db) {
+  __shared__ __attribute__((aligned(16))) float z[64][MR + 4];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, n0 = blockIdx.y * 64, c = blockIdx.x * 256 + lane * 4;
+  for (int u = threadIdx.x; u < 64 * MR; u += kThreads) {
+    const int m = u >> 6, n = u & 63;
+    z[n][m] = m < M && n0 + n < N ? (float)dz[m * ldz + n0 + n] : 0.f;
+  }
+  f32x4 v[MR];
+#pragma unroll
+  for (int m = 0; m < MR; ++m) {
+    typename Four<T>::Raw r = {};
+    if (m < M && c + 4 <= K) r = *reinterpret_cast<const typename Four<T>::Any *>(x + m * ldx + c);
+    else if (m < M) r = piece<T, typename Four<T>::Raw>(x + m * ldx, c, K);
+    v[m] = widen4(r);
+  }
   __syncthreads();
-  const int m = threadIdx.x >> 4, c = threadIdx.x & 15, j = blockIdx.x * 16 + c;
-  if (threadIdx.x >= 256 || m >= a.M || j >= a.N) return;
-  float v = red[0][m][c];
+  if (db && blockIdx.x == 0 && threadIdx.x < 64 && n0 + (int)threadIdx.x < N) {
+    float s = 0.f;
 #pragma unroll
-  for (int s = 1; s < 8; ++s) v += red[s][m][c];
-  finish<T>(a.e, m, j, v, a.e.d.rng ? dropout_base(a.e.d.rng) : 0);
+    for (int m = 0; m < MR; ++m) s += z[threadIdx.x][m];
+    db[n0 + threadIdx.x] = s;
+  }
+  const int left = K - c;
+  for (int r = 0; r < 16; ++r) {
+    const int n = wave * 16 + r;
+    if (n0 + n >= N || left <= 0) break;
+    f32x4 s = {};
+#pragma unroll
+    for (int m = 0; m < MR; m += 4) {
+      const f32x4 q = *reinterpret_cast<const f32x4 *>(&z[n][m]);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) s += q[e] * v[m + e];
+    }
+    float *to = dw + (long long)(n0 + n) * K + c;
+    if (left >= 4) {
+      *reinterpret_cast<f32x4_any *>(to) = s;
+    } else {
+#pragma unroll
+      for (int e = 0; e < 3; ++e)
+        if (e < left) to[e] = s[e];
+    }
+  }
 }
 
 // db on its own: 64 columns of dz to a workgroup, four ranges of rows
@@ -727,7 +882,28 @@ __global__ __launch_bounds__(kThreads) void col_sum_kernel(const T *dz, long lon
 }
 
 // ---- plans ----------------------------------------------------------------------------------------------------------
-constexpr int kFewRows = 16;
+// Up to this many rows go without tiles.  us, 4096 -> 4096, tiles (with what they lay out and join) -> few rows:
+//   fp32 1 row: forward 52 -> 15, data gradient 53 -> 15, weight gradient 33 -> 13      17 rows: 53 -> 20, 55 -> 19, 34 -> as it was
+//   fp32 64 rows: 66 -> 38, 56 -> 40     bf16 1 row: forward 13 -> 7.1 (4.7 TB/s), data gradient 11 -> 40 (64 columns to a workgroup: tiles), weight gradient 27 -> 13 (5.2 TB/s)
+//   bf16 32 rows: forward 13.1 -> 13.7, at 512 -> 512 6.0 -> 3.9
+int few(int dt, int op) {
+  if (op == 2) return 16;
+  return dt == DT_F32 ? 64 : op == 0 ? 32 : 0;
+}
+// Ranges of the reduction: a few hundred workgroups where there are less than one for every other CU, as long as each wave has whole turns of loads.
+struct FewPlan { int wgs, splits, per; };
+FewPlan plan_few(int dt, int op, long long M, int J, int R) {
+  FewPlan p;
+  const int cols = op == 0 ? 16 : 64, groups = M <= 16 ? 1 : M <= 32 ? 2 : 4;
+  const int turn = op == 0 ? 8 * (dt == DT_F32 ? 16 : 32) * (groups == 1 ? 8 : 4) : 8 * 16 * (groups == 4 ? 2 : 4);
+  p.wgs = (J + cols - 1) / cols;
+  p.splits = 1;
+  if (p.wgs < 128) p.splits = std::max(1, std::min(R / turn, 384 / p.wgs));
+  if (p.splits < 3) p.splits = 1;   // a launch more than they save
+  p.per = ((R + p.splits - 1) / p.splits + turn - 1) / turn * turn;
+  p.splits = (R + p.per - 1) / p.per;
+  return p;
+}
 
 // Which tiles, and how many ranges of the reduction (`splits`): the least time by a model of the kernels, us, with what was measured alone on the chip:
 // a launch, then rounds of as many workgroups as fit (one or two a CU), each its start and epilogue and `step` per 64 of the reduction
@@ -738,11 +914,12 @@ constexpr int kFewRows = 16;
 //   128x4096x512, 64x64: 1 split 21.4, 2 14.8, 4 11.2, 8 10.7            128x512x4096, 64x64: 1 split 5.7, 2 9.4, 4 11.5
 //   fp32 2048x1024x4096 (256x128 | 128x128 | 64x64)  100 | 108 | 146     fp32 2000x1024x1024  74 | 49 (2 splits 42) | 47
 struct TileCost { int bm, bn, fit; double start, low, full; };
-constexpr TileCost kTiles[2][3] = {{{256, 256, 256, 7.0, 1.15, 1.58}, {128, 128, 512, 2.6, 0.58, 1.03}, {64, 64, 512, 1.4, 0.28, 0.42}},
+constexpr int kSizes = 3;
+constexpr TileCost kTiles[2][kSizes] = {{{256, 256, 256, 7.0, 1.15, 1.58}, {128, 128, 512, 2.6, 0.58, 1.03}, {64, 64, 512, 1.4, 0.28, 0.42}},
                                    {{256, 128, 256, 5.0, 3.2, 5.0}, {128, 128, 256, 3.0, 1.75, 2.6}, {64, 64, 512, 1.5, 0.81, 2.0}}};
 constexpr double kLaunch = 2.0, kJoin = 3.0, kBytesPerUs = 3.5e6;
 struct Plan {
-  int size;                  // of the tiles: 0 the largest ... 2 the smallest
+  int size;                  // of the tiles: an index into kTiles
   int bm, bn, splits;
   long long per_split;
 };
@@ -750,7 +927,7 @@ Plan plan_tiles(int np, long long I, long long J, long long R) {
   const long long steps = (R + 63) / 64;
   Plan best{};
   double least = 0.;
-  for (int size = 0; size < 3; ++size) {
+  for (int size = 0; size < kSizes; ++size) {
     const TileCost &c = kTiles[np == 3][size];
     const long long tiles = ((I + c.bm - 1) / c.bm) * ((J + c.bn - 1) / c.bn);
     for (const int want : {1, 2, 3, 4, 6, 8, 12, 16, 24, 32}) {
@@ -840,6 +1017,15 @@ template <typename O, bool AR, bool BR, int NP, int BM, int BN, int BK, int STAG
   return RESIST_OK;
 }
 
+template <typename O> int join(const JoinArgs &j, hipStream_t st) {
+  const long long wgs = j.sum_wgs + (j.splits > 1 ? (j.I * ((j.J + 7) / 8) + kThreads - 1) / kThreads : 0);
+  if (wgs > 0x7fffffffLL) return set_error(RESIST_ESHAPE, "linear: too many outputs");
+  prof::Scope sc("linear_join", 0., j.splits > 1 ? (double)j.splits * j.I * j.J * 4 : 0., st);
+  gemm_join_kernel<O><<<(unsigned)wgs, kThreads, 0, st>>>(j);
+  RESIST_CHECK_LAUNCH("linear_join");
+  return RESIST_OK;
+}
+
 // the product of a call, its operands laid out first where they have to be, what was split joined after
 template <typename O, int NP, bool AR, bool BR>
 int product(const Layout &l, const void *a, const void *b, long long I, int J, long long R, const Epilogue &e, float *db, void *work, const char *name,
@@ -892,21 +1078,49 @@ int product(const Layout &l, const void *a, const void *b, long long I, int J, l
   JoinArgs j{};
   j.part = t.part; j.splits = t.splits; j.I = I; j.J = J; j.e = e;
   j.sums = sums; j.db = db; j.sum_parts = l.sum_parts; j.sum_n = (int)I; j.sum_wgs = db ? (int)((I + 63) / 64) : 0;
-  const long long wgs = j.sum_wgs + (t.splits > 1 ? (I * ((J + 7) / 8) + kThreads - 1) / kThreads : 0);
-  if (wgs > 0x7fffffffLL) return set_error(RESIST_ESHAPE, "linear: too many outputs");
-  prof::Scope sc("linear_join", 0., t.splits > 1 ? (double)t.splits * I * J * 4 : 0., st);
-  gemm_join_kernel<O><<<(unsigned)wgs, kThreads, 0, st>>>(j);
-  RESIST_CHECK_LAUNCH("linear_join");
-  return RESIST_OK;
+  return join<O>(j, st);
 }
 
 double flops_of(const LinearShape &s) { return 2. * s.M * s.N * s.K; }
+// forward (op 0) or data gradient (op 1, fp32) of few rows
+int few_rows(const LinearShape &s, int dt, int op, const void *a, int64_t lda, const void *w, const Epilogue &e, void *work, const char *name, double bytes, hipStream_t st) {
+  const int J = op == 0 ? s.N : s.K;
+  const FewPlan p = plan_few(dt, op, s.M, J, op == 0 ? s.K : s.N);
+  const FewArgs f{a, w, lda, (int)s.M, s.K, s.N, p.splits, p.per, static_cast<float *>(work), e};
+  const dim3 wgs(p.wgs, p.splits);
+  {
+    prof::Scope sc(name, flops_of(s), bytes, st);
+    if (op == 1) {
+      if (s.M <= 16) few_rows_dgrad_kernel<1><<<wgs, 512, 0, st>>>(f);
+      else if (s.M <= 32) few_rows_dgrad_kernel<2><<<wgs, 512, 0, st>>>(f);
+      else few_rows_dgrad_kernel<4><<<wgs, 512, 0, st>>>(f);
+    } else if (dt == DT_F32) {
+      if (s.M <= 16) few_rows_fwd_kernel<float, 1><<<wgs, 512, 0, st>>>(f);
+      else if (s.M <= 32) few_rows_fwd_kernel<float, 2><<<wgs, 512, 0, st>>>(f);
+      else few_rows_fwd_kernel<float, 4><<<wgs, 512, 0, st>>>(f);
+    } else {
+      if (s.M <= 16) few_rows_fwd_kernel<__bf16, 1><<<wgs, 512, 0, st>>>(f);
+      else few_rows_fwd_kernel<__bf16, 2><<<wgs, 512, 0, st>>>(f);
+    }
+    RESIST_CHECK_LAUNCH(name);
+  }
+  if (p.splits == 1) return RESIST_OK;
+  JoinArgs j{};
+  j.part = f.part; j.splits = p.splits; j.I = s.M; j.J = J; j.e = e;
+  return dt == DT_F32 ? join<float>(j, st) : join<__bf16>(j, st);
+}
 double bytes_of(const LinearShape &s, int dt, double outs) { return ((double)s.M * s.K + (double)s.N * s.K + (double)s.M * s.N) * esize(dt) + outs; }
 
 }  // namespace
 
 int64_t linear_workspace(const LinearShape &s, int dt, int op) {
-  if (s.M == 0 || (op == 0 && s.M <= kFewRows)) return 0;
+  if (s.M == 0) return 0;
+  if (s.M <= few(dt, op)) {
+    if (op == 2) return 0;
+    const int J = op == 0 ? s.N : s.K;
+    const FewPlan p = plan_few(dt, op, s.M, J, op == 0 ? s.K : s.N);
+    return p.splits > 1 ? align256((int64_t)p.splits * s.M * J * 4) : 0;
+  }
   return layout_of(s, dt, op).bytes;
 }
 
@@ -916,14 +1130,7 @@ int linear_fwd(const LinearShape &s, int dt, const void *x, const void *w, const
   e.out = y; e.ldo = s.ldy; e.bias = le.bias; e.z_out = le.z; e.ldz = le.ldz; e.res = le.residual; e.ldr = le.ldr; e.act = le.act;
   e.d = make_dropout(le.drop); e.words = (s.N + 1) / 2;
   const double bytes = bytes_of(s, dt, (double)s.M * s.N * esize(dt) * ((le.z != nullptr) + (le.residual != nullptr)));
-  if (s.M <= kFewRows) {
-    const FewArgs f{x, w, s.ldx, (int)s.M, s.K, s.N, e};
-    prof::Scope sc("linear_few_rows", flops_of(s), bytes, st);
-    if (dt == DT_F32) few_rows_kernel<float><<<(s.N + 15) / 16, 512, 0, st>>>(f);
-    else few_rows_kernel<__bf16><<<(s.N + 15) / 16, 512, 0, st>>>(f);
-    RESIST_CHECK_LAUNCH("linear_few_rows");
-    return RESIST_OK;
-  }
+  if (s.M <= few(dt, 0)) return few_rows(s, dt, 0, x, s.ldx, w, e, work, "linear_few_rows_fwd", bytes, st);
   const Layout l = layout_of(s, dt, 0);
   return dt == DT_F32 ? product<float, 3, true, true>(l, x, w, s.M, s.N, s.K, e, nullptr, work, "linear_fwd", flops_of(s), bytes, st)
                       : product<__bf16, 1, true, true>(l, x, w, s.M, s.N, s.K, e, nullptr, work, "linear_fwd", flops_of(s), bytes, st);
@@ -934,8 +1141,9 @@ int linear_dgrad(const LinearShape &s, int dt, const void *dz, const void *w, co
   Epilogue e{};
   e.out = dx; e.ldo = s.ldx; e.z_in = lt.act == RESIST_ACT_NONE ? nullptr : lt.z; e.ldz = lt.ldz; e.act = lt.act;
   e.d = make_dropout(lt.drop); e.words = (s.K + 1) / 2;
-  const Layout l = layout_of(s, dt, 1);
   const double bytes = bytes_of(s, dt, e.z_in ? (double)s.M * s.K * esize(dt) : 0.);
+  if (s.M <= few(dt, 1)) return few_rows(s, dt, 1, dz, s.ldy, w, e, work, "linear_few_rows_dgrad", bytes, st);
+  const Layout l = layout_of(s, dt, 1);
   return dt == DT_F32 ? product<float, 3, true, false>(l, dz, w, s.M, s.K, s.N, e, nullptr, work, "linear_dgrad", flops_of(s), bytes, st)
                       : product<__bf16, 1, true, false>(l, dz, w, s.M, s.K, s.N, e, nullptr, work, "linear_dgrad", flops_of(s), bytes, st);
 }
@@ -949,10 +1157,28 @@ int linear_wgrad(const LinearShape &s, int dt, const void *dz, const void *x, fl
     RESIST_CHECK_LAUNCH("linear_bias");
     return RESIST_OK;
   }
+  const double bytes = ((double)s.M * s.K + (double)s.M * s.N) * esize(dt) + 4. * s.N * s.K;
+  if (s.M <= few(dt, 2)) {
+    const dim3 wgs((s.K + 255) / 256, (s.N + 63) / 64);
+    const int M = (int)s.M;
+    prof::Scope sc("linear_few_rows_wgrad", flops_of(s), bytes, st);
+    auto launch = [&](auto kernel, auto type) {
+      typedef decltype(type) T;
+      kernel<<<wgs, kThreads, 0, st>>>(static_cast<const T *>(dz), s.ldy, static_cast<const T *>(x), s.ldx, M, s.N, s.K, dw, db);
+    };
+    if (dt == DT_F32) {
+      if (M <= 4) launch(few_rows_wgrad_kernel<float, 4>, float{});
+      else launch(few_rows_wgrad_kernel<float, 16>, float{});
+    } else {
+      if (M <= 4) launch(few_rows_wgrad_kernel<__bf16, 4>, __bf16{});
+      else launch(few_rows_wgrad_kernel<__bf16, 16>, __bf16{});
+    }
+    RESIST_CHECK_LAUNCH("linear_few_rows_wgrad");
+    return RESIST_OK;
+  }
   Epilogue e{};
   e.out = dw; e.ldo = s.K;
   const Layout l = layout_of(s, dt, 2);
-  const double bytes = ((double)s.M * s.K + (double)s.M * s.N) * esize(dt) + 4. * s.N * s.K;
   return dt == DT_F32 ? product<float, 3, false, false>(l, dz, x, s.N, s.K, s.M, e, db, work, "linear_wgrad", flops_of(s), bytes, st)
                       : product<float, 1, false, false>(l, dz, x, s.N, s.K, s.M, e, db, work, "linear_wgrad", flops_of(s), bytes, st);
 }

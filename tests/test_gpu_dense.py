@@ -214,7 +214,7 @@ def test_activation_of_a_dense_layer(act, dt):
 
 # ---- dense layers --------------------------------------------------------------------------------------------------
 SHAPES = [(1, 1, 1), (1, 64, 64), (2, 8, 16), (3, 5, 7), (1, 4096, 1000), (8, 1000, 520), (17, 100, 33), (16, 513, 64), (64, 64, 64), (130, 257, 129), (128, 2049, 40), (333, 1000, 515),
-          (256, 512, 384), (70, 24, 2056), (600, 40, 72), (1030, 520, 264), (515, 1032, 776), (100, 96, 4000), (5, 3000, 6)]
+          (256, 512, 384), (70, 24, 2056), (600, 40, 72), (1030, 520, 264), (515, 1032, 776), (100, 96, 4000), (5, 3000, 6), (3, 8200, 24), (40, 4100, 70), (30, 70, 5000), (12, 65, 9001), (33, 2048, 64)]
 
 
 def sums(a, b, n):
