@@ -51,7 +51,8 @@ __device__ inline void finish(const Epilogue &e, long long i, int j, float v, u6
 
 // ---- operands in the workspace --------------------------------------------------------------------------------------
 // A matrix [rows][n] with `ld` elements between rows becomes [rows][to_ld] of bf16, to_ld a multiple of eight, with zeros behind a row's end:
-// a copy (bf16), or three planes of parts (fp32).  Of parts, each 64x64 block also leaves a word: whether it has a value that three parts
+// a copy (bf16), or three planes of parts (fp32).  Parts whose rows are the reduction's axis lie [to_ld/32][rows][32], to_ld a multiple of 32: the
+// tiles read them 32 at a time, of which a row's 64 bytes would be half a line each.  Of parts, each 64x64 block also leaves a word: whether it has a value that three parts
 // do not hold (conv3.hip: not finite or rounding to infinity, or below 2^-110).
 struct LayOut {
   const void *from;
@@ -59,7 +60,7 @@ struct LayOut {
   unsigned *flags;          // [ceil(rows/64)][ceil(to_ld/64)]
   float *sums;              // optional [ceil(rows/64)][n]: of the columns, 64 rows each
   long long rows, ld, plane;   // plane: elements between planes
-  int n, to_ld, blocks_n, blocks;
+  int n, to_ld, blocks_n, blocks, panels;   // panels: [to_ld/32][rows][32]
 };
 struct LayOutArgs { LayOut m[2]; };
 // split_check, and for NaN: what two parts leave of a value that is not finite or rounds to infinity
@@ -87,7 +88,7 @@ __global__ __launch_bounds__(kThreads) void lay_out_kernel(LayOutArgs a) {
     if (row >= m.rows || c >= m.to_ld) continue;
     float v[8];
     row_load(static_cast<const T *>(m.from) + row * m.ld + c, m.n - c, v);
-    __bf16 *to = m.to + row * m.to_ld + c;
+    __bf16 *to = m.to + (m.panels ? ((long long)(c >> 5) * m.rows + row) * 32 + (c & 31) : row * m.to_ld + c);
     if constexpr (NP == 3) {
 #pragma unroll
       for (int e = 0; e < 8; ++e) sum[e] += v[e];
@@ -278,20 +279,22 @@ __global__ __launch_bounds__(kThreads, WGS) void gemm_tile_kernel(TileArgs g) {
   const int steps = (int)((rend - rbeg + BK - 1) / BK);
 
   // ---- operands to LDS.  left: bytes from the tile's current corner to the operand's end
-  const char *pa = reinterpret_cast<const char *>(g.a + (AR ? i0 * g.lda + rbeg : rbeg * g.lda + i0));
-  const char *pb = reinterpret_cast<const char *>(g.b + (BR ? (long long)j0 * g.ldb + rbeg : rbeg * g.ldb + j0));
-  long long left_a = AR ? ((g.I - i0 - 1) * g.lda + (rend - rbeg + 7) / 8 * 8) * 2 : ((rend - rbeg - 1) * g.lda + (g.I - i0 + 7) / 8 * 8) * 2;
-  long long left_b = BR ? ((g.J - j0 - 1) * g.ldb + (rend - rbeg + 7) / 8 * 8) * 2 : ((rend - rbeg - 1) * g.ldb + (g.J - j0 + 7) / 8 * 8) * 2;
+  constexpr bool PA = AR && NP == 3, PB = BR && NP == 3;   // in panels of 32 steps: [R/32][I][32]
+  static_assert(NP == 1 || BK == 32, "panels");
+  const char *pa = reinterpret_cast<const char *>(g.a + (PA ? (rbeg >> 5) * g.I * 32 + i0 * 32 : AR ? i0 * g.lda + rbeg : rbeg * g.lda + i0));
+  const char *pb = reinterpret_cast<const char *>(g.b + (PB ? (rbeg >> 5) * g.J * 32 + (long long)j0 * 32 : BR ? (long long)j0 * g.ldb + rbeg : rbeg * g.ldb + j0));
+  long long left_a = PA ? (g.I - i0) * 64 : AR ? ((g.I - i0 - 1) * g.lda + (rend - rbeg + 7) / 8 * 8) * 2 : ((rend - rbeg - 1) * g.lda + (g.I - i0 + 7) / 8 * 8) * 2;
+  long long left_b = PB ? (long long)(g.J - j0) * 64 : BR ? ((g.J - j0 - 1) * g.ldb + (rend - rbeg + 7) / 8 * 8) * 2 : ((rend - rbeg - 1) * g.ldb + (g.J - j0 + 7) / 8 * 8) * 2;
   unsigned va[SA::kLoads], vb[SB::kLoads];
 #pragma unroll
   for (int p = 0; p < SA::kLoads; ++p) {
     const int r = SA::row(p, wave, lane);
-    va[p] = (unsigned)(r * g.lda * 2) + SA::piece(r, lane) * 16;
+    va[p] = (PA ? r * 64u : (unsigned)(r * g.lda * 2)) + SA::piece(r, lane) * 16;
   }
 #pragma unroll
   for (int p = 0; p < SB::kLoads; ++p) {
     const int r = SB::row(p, wave, lane);
-    vb[p] = (unsigned)(r * g.ldb * 2) + SB::piece(r, lane) * 16;
+    vb[p] = (PB ? r * 64u : (unsigned)(r * g.ldb * 2)) + SB::piece(r, lane) * 16;
   }
   // of a row of BK reduction steps: the first step of this lane's piece (the same in every instruction)
   const int ka = SA::piece(SA::row(0, wave, lane), lane) * 8, kb = SB::piece(SB::row(0, wave, lane), lane) * 8;
@@ -307,9 +310,11 @@ __global__ __launch_bounds__(kThreads, WGS) void gemm_tile_kernel(TileArgs g) {
     transfer(r, v, lds_at + stage * kStage + (is_a ? 0 : kA) + q * 4096);
   };
   auto advance = [&]() {
-    const long long da = (AR ? BK : BK * g.lda) * 2, db = (BR ? BK : BK * g.ldb) * 2;
-    pa += da; left_a -= da;
-    pb += db; left_b -= db;
+    const long long da = PA ? g.I * 64 : (AR ? BK : BK * g.lda) * 2, db = PB ? g.J * 64LL : (BR ? BK : BK * g.ldb) * 2;
+    pa += da;
+    pb += db;
+    if constexpr (!PA) left_a -= da;   // (of panels, what is past the reduction's end is not asked for)
+    if constexpr (!PB) left_b -= db;
     left_r -= BK;
   };
 
@@ -916,7 +921,7 @@ FewPlan plan_few(int dt, int op, long long M, int J, int R) {
 struct TileCost { int bm, bn, fit; double start, low, full; };
 constexpr int kSizes = 3;
 constexpr TileCost kTiles[2][kSizes] = {{{256, 256, 256, 7.0, 1.15, 1.58}, {128, 128, 512, 2.6, 0.58, 1.03}, {64, 64, 512, 1.4, 0.28, 0.42}},
-                                   {{256, 128, 256, 5.0, 3.2, 5.0}, {128, 128, 256, 3.0, 1.75, 2.6}, {64, 64, 512, 1.5, 0.81, 2.0}}};
+                                   {{256, 128, 256, 5.0, 2.9, 4.6}, {128, 128, 256, 3.0, 1.6, 2.4}, {64, 64, 512, 1.5, 0.65, 1.55}}};
 constexpr double kLaunch = 2.0, kJoin = 3.0, kBytesPerUs = 3.5e6;
 struct Plan {
   int size;                  // of the tiles: an index into kTiles
@@ -950,7 +955,7 @@ Plan plan_tiles(int np, long long I, long long J, long long R) {
 struct Operand {
   long long rows, ld;
   int n;
-  bool moved;
+  bool moved, panels;
   long long to_ld, plane;    // as the kernel reads it
   int64_t at, flags_at;      // bytes into the workspace
 };
@@ -965,10 +970,11 @@ int64_t align256(int64_t n) { return (n + 255) & ~(int64_t)255; }
 int64_t blocks64(long long rows, long long n) { return ((rows + 63) / 64) * ((n + 63) / 64); }
 // `whole`: the reduction is the contiguous axis, so that a row's end has to be one of eight elements
 Operand operand(int dt, long long rows, int n, long long ld, bool whole, int64_t *at) {
-  Operand o{rows, ld, n, false, ld, 0, 0, 0};
+  Operand o{rows, ld, n, false, false, ld, 0, 0, 0};
   o.moved = dt == DT_F32 || ld % 8 != 0 || (whole && n % 8 != 0);
   if (!o.moved) return o;
-  o.to_ld = (n + 7) / 8 * 8;
+  o.panels = dt == DT_F32 && whole;
+  o.to_ld = o.panels ? (n + 31) / 32 * 32 : (n + 7) / 8 * 8;
   o.plane = rows * o.to_ld;
   o.at = *at;
   *at += align256(o.plane * 2 * (dt == DT_F32 ? 3 : 1));
@@ -1039,7 +1045,7 @@ int product(const Layout &l, const void *a, const void *b, long long I, int J, l
     auto add = [&](const Operand &o, const void *from, float *to_sums) {
       if (!o.moved) return;
       LayOut &m = args.m[n++];
-      m = LayOut{from, reinterpret_cast<__bf16 *>(ws + o.at), reinterpret_cast<unsigned *>(ws + o.flags_at), to_sums, o.rows, o.ld, o.plane, o.n, (int)o.to_ld, 0, 0};
+      m = LayOut{from, reinterpret_cast<__bf16 *>(ws + o.at), reinterpret_cast<unsigned *>(ws + o.flags_at), to_sums, o.rows, o.ld, o.plane, o.n, (int)o.to_ld, 0, 0, o.panels};
       m.blocks_n = (o.n + 63) / 64;
       m.blocks = (int)((o.rows + 63) / 64 * m.blocks_n);
       moved += (NP == 3 ? 10. : 4.) * o.rows * o.n;
