@@ -143,7 +143,7 @@ int resist_dropout_backward(int64_t M, int32_t N, int32_t dtype, const void *dy,
  *   forward          z = x w' + bias,  y = [residual +] drop(act(z))      [y in place of residual]
  *   data gradient    dx = a'(z) drop(dz w): z, act and drop are of the layer that produced x, the gradient leaves taken
  *                    through them                                         [dx in place of z]
- *   weight gradient  dw = dz' x [N][K], db = column sums of dz [N]; either may be NULL
+ *   weight gradient  dw = dz' x [N][K], db = column sums of dz [N]; db may be NULL
  * dz and y share ldy, dx and x share ldx.
  * Workspace (may be NULL where resist_linear_workspace_bytes is 0): operands laid out for the kernels, and partial sums; calls
  * that overlap in time need one each.  op: 0 forward, 1 data gradient, 2 weight gradient.  It depends on the shape alone.

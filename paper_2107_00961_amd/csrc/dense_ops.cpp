@@ -176,14 +176,14 @@ extern "C" int resist_linear_wgrad(const resist_linear_shape *s, const void *dz,
                                    int64_t workspace_bytes, void *hip_stream) {
   LinearShape l;
   RESIST_TRY(to_linear(s, &l));
-  RESIST_TRY(check_ptr(dw, "dw", false));
+  RESIST_TRY(check_ptr(dw, "dw"));
   RESIST_TRY(check_ptr(db, "db", false));
   if (l.M == 0) {   // no rows: the gradients are there, and zero
-    if (dw) RESIST_TRY(fill_zero_f32(dw, (int64_t)l.N * l.K, (hipStream_t)hip_stream));
+    RESIST_TRY(fill_zero_f32(dw, (int64_t)l.N * l.K, (hipStream_t)hip_stream));
     return db ? fill_zero_f32(db, l.N, (hipStream_t)hip_stream) : RESIST_OK;
   }
   RESIST_TRY(check_ptr(dz, "dz"));
-  if (dw) RESIST_TRY(check_ptr(x, "x"));
+  RESIST_TRY(check_ptr(x, "x"));
   RESIST_TRY(check_work(l, s->dtype, 2, workspace, workspace_bytes));
   return linear_wgrad(l, s->dtype, dz, x, dw, db, workspace, (hipStream_t)hip_stream);
 }

@@ -873,19 +873,6 @@ __global__ __launch_bounds__(kThreads) void few_rows_wgrad_kernel(const T *dz, l
   }
 }
 
-// db on its own: 64 columns of dz to a workgroup, four ranges of rows
-template <typename T>
-__global__ __launch_bounds__(kThreads) void col_sum_kernel(const T *dz, long long M, int N, long long ld, float *db) {
-  __shared__ double red[4][64];
-  const int c = blockIdx.x * 64 + (threadIdx.x & 63), k = threadIdx.x >> 6;
-  double s = 0.;
-  if (c < N)
-    for (long long m = k; m < M; m += 4) s += (double)(float)dz[m * ld + c];
-  red[k][threadIdx.x & 63] = s;
-  __syncthreads();
-  if (k == 0 && c < N) db[c] = (float)(((red[0][threadIdx.x] + red[1][threadIdx.x]) + red[2][threadIdx.x]) + red[3][threadIdx.x]);
-}
-
 // ---- plans ----------------------------------------------------------------------------------------------------------
 // Up to this many rows go without tiles.  us, 4096 -> 4096, tiles (with what they lay out and join) -> few rows:
 //   fp32 1 row: forward 52 -> 15, data gradient 53 -> 15, weight gradient 33 -> 13      17 rows: 53 -> 20, 55 -> 19, 34 -> as it was
@@ -1036,6 +1023,7 @@ template <typename O> int join(const JoinArgs &j, hipStream_t st) {
 template <typename O, int NP, bool AR, bool BR>
 int product(const Layout &l, const void *a, const void *b, long long I, int J, long long R, const Epilogue &e, float *db, void *work, const char *name,
             double flops, double bytes, hipStream_t st) {
+  if (blocks64(l.a.rows, l.a.n) + blocks64(l.b.rows, l.b.n) > 0x7fffffff) return set_error(RESIST_ESHAPE, "linear: too many rows and columns");
   char *ws = static_cast<char *>(work);
   float *sums = db ? reinterpret_cast<float *>(ws + l.sums_at) : nullptr;
   if (l.a.moved || l.b.moved) {
@@ -1052,8 +1040,9 @@ int product(const Layout &l, const void *a, const void *b, long long I, int J, l
     };
     add(l.a, a, NP == 3 ? sums : nullptr);
     add(l.b, b, nullptr);
+    const long long wgs = (long long)args.m[0].blocks + args.m[1].blocks;
     prof::Scope sc("linear_lay_out", 0., moved, st);
-    lay_out_kernel<NP><<<args.m[0].blocks + args.m[1].blocks, kThreads, 0, st>>>(args);
+    lay_out_kernel<NP><<<(unsigned)wgs, kThreads, 0, st>>>(args);
     RESIST_CHECK_LAUNCH("linear_lay_out");
   }
   TileArgs t{};
@@ -1155,14 +1144,6 @@ int linear_dgrad(const LinearShape &s, int dt, const void *dz, const void *w, co
 }
 
 int linear_wgrad(const LinearShape &s, int dt, const void *dz, const void *x, float *dw, float *db, void *work, hipStream_t st) {
-  if (!dw) {
-    if (!db) return RESIST_OK;
-    prof::Scope sc("linear_bias", 0., (double)s.M * s.N * esize(dt), st);
-    if (dt == DT_F32) col_sum_kernel<float><<<(s.N + 63) / 64, kThreads, 0, st>>>(static_cast<const float *>(dz), s.M, s.N, s.ldy, db);
-    else col_sum_kernel<__bf16><<<(s.N + 63) / 64, kThreads, 0, st>>>(static_cast<const __bf16 *>(dz), s.M, s.N, s.ldy, db);
-    RESIST_CHECK_LAUNCH("linear_bias");
-    return RESIST_OK;
-  }
   const double bytes = ((double)s.M * s.K + (double)s.M * s.N) * esize(dt) + 4. * s.N * s.K;
   if (s.M <= few(dt, 2)) {
     const dim3 wgs((s.K + 255) / 256, (s.N + 63) / 64);

@@ -292,6 +292,49 @@ def test_linear_wgrad(m, k, n, dt):
     assert torch.equal(dw, again[0]) and torch.equal(db, again[1])
 
 
+# every size of tile, with ragged edges on all sides, whole and split reductions (the largest tiles: the second forward, the last in all three in bf16)
+LARGE = [(4000, 264, 4104), (5000, 200, 3001), (2050, 521, 8000), (4100, 520, 4360), (1100, 2050, 2000), (300, 4090, 2100), (3990, 3000, 4090)]
+
+
+def product64(a, b):
+    return host(torch.from_numpy(a).cuda() @ torch.from_numpy(np.ascontiguousarray(b)).cuda())
+
+
+def large_sums(a, b, n):
+    return (4 * np.sqrt(n) + 4) * U * product64(np.abs(a), np.abs(b))
+
+
+@pytest.mark.parametrize("dt", ["f32", "bf16"])
+@pytest.mark.parametrize("m,k,n", LARGE)
+def test_linear_large(m, k, n, dt):
+    print("linear_large", m, k, n, dt, flush=True)
+    x, w, b, res, z = lin_data(m, k, n, m)
+    wd, w64 = rounded(w, dt)
+    xd, x64 = apart(x, dt, 8)
+    rd, r64 = apart(res, dt, 3)
+    zd, z64 = rounded(z, dt)
+    act = ACTS[1 + m // 10 % 4]
+    want = product64(x64, w64.T) + b
+    e = large_sums(x64, w64.T, k)
+    near(R.linear_forward(xd, wd, dev(b)), want, e + 2 * U * np.abs(want) + HALF[dt] * 1.01 * np.abs(want), "forward")
+    y, zo = R.linear_forward(xd, wd, dev(b), act=act, p=0.25, rng=rng_tensor(7, 9), residual=rd, keep_z=True)
+    near(zo, want, e + 2 * U * np.abs(want) + HALF[dt] * 1.01 * np.abs(want), "z")
+    a = np.where(D.kept((7, 9), m, n, 0.25), D.act(want, act) / 0.75, 0.0)
+    near(y, a + r64, (1.2 * e + 16 * U * np.minimum(np.abs(want), 20)) / 0.75 + 6 * U * np.abs(a) + (U + HALF[dt] * 1.01) * np.abs(a + r64), "forward, everything")
+    # gradients: of rows `res`
+    want = product64(r64, w64)
+    e = large_sums(r64, w64, n)
+    near(R.linear_dgrad(rd, wd), want, e + HALF[dt] * 1.01 * np.abs(want), "dgrad")
+    v = np.where(D.kept((4, 4), m, k, 0.25), want / 0.75, 0.0)
+    s = D.slope(z64, act)
+    near(R.linear_dgrad(rd, wd, act=act, z=zd, p=0.25, rng=rng_tensor(4, 4)), v * s,
+         1.2 * e / 0.75 + np.abs(v) * 16 * U * np.maximum(1, np.abs(z64)) + (4 * U + HALF[dt] * 1.01) * np.abs(v * s), "dgrad through")
+    dw, db = R.linear_wgrad(rd, xd)
+    near(dw, product64(r64.T, x64), large_sums(r64.T, x64, m), "dw")
+    near(db, r64.sum(0), (4 * np.sqrt(m) + 4) * U * np.abs(r64).sum(0), "db")
+    assert all(torch.equal(p, q) for p, q in zip((dw, db), R.linear_wgrad(rd, xd)))
+
+
 def test_no_rows():
     x, w = torch.empty(0, 24, device="cuda"), torch.ones(16, 24, device="cuda")
     assert R.linear_forward(x, w).shape == (0, 16) and R.linear_dgrad(torch.empty(0, 16, device="cuda"), w).shape == (0, 24)
@@ -332,6 +375,15 @@ def test_fp32_operands_over_their_whole_range():
         xd, x64 = rounded((x * np.float32(sx)).astype(np.float32), "f32")
         wd, w64 = rounded((w * np.float32(sw)).astype(np.float32), "f32")
         near(R.linear_forward(xd, wd), x64 @ w64.T, sums(x64, w64.T, k), f"{sx} {sw}")
+    # in tiles of every size: one value that three bf16 parts do not hold among ordinary ones
+    for m, k, n in ((140, 72, 136), (1500, 320, 2600), (5000, 200, 3000)):
+        x, w, *_ = lin_data(m, k, n, 6)
+        x[m // 2, k // 2], w[n // 3, 5] = 2.0 ** -125, 3.4e38
+        xd, x64 = rounded(x, "f32")
+        wd, w64 = rounded(w * np.float32(2.0 ** -3), "f32")
+        near(R.linear_forward(xd, wd), x64 @ w64.T, sums(x64, w64.T, k), f"{m} {k} {n}")
+        dw, _ = R.linear_wgrad(R.linear_forward(xd, wd)[:, :n], xd)
+        assert torch.isfinite(dw[: n // 3]).all()
     xd = torch.full((130, 8), 0.0, device="cuda")
     xd[:, 0] = 3.4e38                                          # a float just below the largest, kept as it is
     wd = torch.zeros(128, 8, device="cuda")

@@ -78,7 +78,6 @@ def test_no_rows_is_no_work():
     assert ln_bwd(M=0, dy=None, x=None, dx=None, mean=None, rstd=None, dg=None, db=None, ws=None, n=0) == 0
     assert drop_fwd(M=0, x=None, y=None) == 0 and drop_bwd(M=0, dy=None, z=None, dx=None) == 0
     assert linear(0, M=0, x=None, w=None, y=None) == 0 and linear(1, M=0, x=None, w=None, y=None) == 0
-    assert linear(2, M=0, x=None, y=None, dw=None, db=None) == 0
 
 
 def linear(op, M=4, K=8, N=8, ldx=0, ldy=0, dt=0, x=P, w=P, y=P, dw=P, db=P, ws=P, n=1 << 40, **e):
@@ -109,7 +108,7 @@ def test_linear_epilogue_refusals():
         assert linear(op, act=2, z=P, ldz=7) == ESHAPE and linear(op, act=2, z=P + 2) == EINVAL
     assert linear(0, bias=P + 4) == EINVAL and linear(0, residual=P + 4) == EINVAL and linear(0, residual=P, ldr=7) == ESHAPE
     assert linear(1, act=2) == EINVAL                                      # an activation's gradient without z
-    assert linear(2, dw=P + 4) == EINVAL and linear(2, db=P + 4) == EINVAL
+    assert linear(2, dw=P + 4) == EINVAL and linear(2, db=P + 4) == EINVAL and linear(2, dw=None) == EINVAL and linear(2, M=0, dw=None) == EINVAL
     n = C.c_int64()
     sh = B._LinearShape(4, 8, 8, 0, 0, 0)
     L = R.lib()
