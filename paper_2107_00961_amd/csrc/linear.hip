@@ -36,7 +36,7 @@ __device__ inline void finish(const Epilogue &e, long long i, int j, float v, u6
   float t[1] = {v};
   if (e.bias) t[0] += e.bias[j];
   if (e.z_out) static_cast<T *>(e.z_out)[i * e.ldz + j] = (T)t[0];
-  if (!e.z_in) activate<1>(t, e.act);
+  if (!e.z_in) activate<sizeof(T) == 2>(t, e.act);
   if (e.d.rng) {
     const u64 w = splitmix(base + ((u64)i * (unsigned)e.words + (unsigned)(j >> 1)) * kGolden);
     t[0] = (unsigned)(j & 1 ? w >> 32 : w) < e.d.thr ? 0.f : t[0] * e.d.scale;
@@ -174,7 +174,7 @@ __device__ inline void finish8(const Epilogue &e, O *out, O *z_out, u64 word, in
 #pragma unroll
   for (int k = 0; k < 8; ++k) v[k] += bias[k];
   if (e.z_out) row_store(z_out, left, v);
-  if (!e.z_in) activate(v, e.act);
+  if (!e.z_in) activate<sizeof(O) == 2>(v, e.act);
   if (e.d.rng) dropout8(base, word, e.d.thr, e.d.scale, v);
   if (e.z_in || e.res) {
     float s[8];
