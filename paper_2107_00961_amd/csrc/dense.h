@@ -104,9 +104,8 @@ inline Dropout make_dropout(const DropSpec &s) {
 }
 // what a word's number is added to: word c is splitmix(base + c * golden)
 __device__ inline u64 dropout_base(const u64 *rng) { return splitmix(rng[0] + kGolden) + (rng[1] + 1) * kGolden; }
-// elements j .. j+7 of a row (j even) whose first word is number `word`
-__device__ inline void dropout8(u64 base, u64 word, unsigned thr, float scale, float (&v)[8]) {
-  u64 at = base + word * kGolden;
+// elements j .. j+7 of a row (j even), the first word's number times golden added to the base
+__device__ inline void dropout8(u64 at, unsigned thr, float scale, float (&v)[8]) {
 #pragma unroll
   for (int i = 0; i < 4; ++i, at += kGolden) {
     const u64 w = splitmix(at);

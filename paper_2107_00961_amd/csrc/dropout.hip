@@ -35,7 +35,7 @@ __global__ __launch_bounds__(kThreads) void dropout_kernel(DropArgs a) {
     row_load(static_cast<const T *>(a.x) + row * a.ldx + c, left, v);
     if (a.res) row_load(static_cast<const T *>(a.res) + row * a.ldr + c, left, o);
     if (a.z) row_load(static_cast<const T *>(a.z) + row * a.ldz + c, left, o);
-    if (a.d.rng) dropout8(base, (u64)row * (unsigned)a.words + (unsigned)(c >> 1), a.d.thr, a.d.scale, v);
+    if (a.d.rng) dropout8(base + ((u64)row * (unsigned)a.words + (unsigned)(c >> 1)) * kGolden, a.d.thr, a.d.scale, v);
     if (a.z) times_slope(v, o, a.act);
     if (a.res) {
 #pragma unroll

@@ -167,26 +167,47 @@ struct TileArgs {
   Epilogue e;
 };
 
-// Eight outputs of a row, at `out`; z goes to `z_out` (optional), `word` is the number of the dropout's first word.  bias: of their columns; side: what
-// the epilogue reads beside them, z (data gradient) or the residual (forward)
-template <typename O>
-__device__ inline void finish8(const Epilogue &e, O *out, O *z_out, u64 word, int left, float (&v)[8], const float (&bias)[8], const Raw8<O> &side, u64 base) {
+// Eight outputs of each of H rows (those that are `ok`), at `out`; z goes to `z_out` (optional), `word` is where the dropout's sequence is for them.  bias: of
+// their columns; side: what the epilogue reads beside them, z (data gradient) or the residual (forward).  Several rows at once, as every
+// branch costs a wave that has its SIMD to itself as much as a dozen instructions.
+template <typename O, int H>
+__device__ inline void finish_rows(const Epilogue &e, O *const (&out)[H], O *const (&z_out)[H], const u64 (&word)[H], int left, const bool (&ok)[H], float (&v)[H][8],
+                                   const float (&bias)[8], const Raw8<O> (&side)[H]) {
 #pragma unroll
-  for (int k = 0; k < 8; ++k) v[k] += bias[k];
-  if (e.z_out) row_store(z_out, left, v);
-  if (!e.z_in) activate<sizeof(O) == 2>(v, e.act);
-  if (e.d.rng) dropout8(base, word, e.d.thr, e.d.scale, v);
-  if (e.z_in || e.res) {
-    float s[8];
-    widen(side, s);
-    if (e.z_in) {
-      times_slope(v, s, e.act);
+  for (int h = 0; h < H; ++h)
+#pragma unroll
+    for (int k = 0; k < 8; ++k) v[h][k] += bias[k];
+  auto store = [&](O *const (&to)[H]) {
+    if (left >= 8) {
+#pragma unroll
+      for (int h = 0; h < H; ++h)
+        if (ok[h]) Row<O>::store(to[h], v[h]);
     } else {
 #pragma unroll
-      for (int k = 0; k < 8; ++k) v[k] += s[k];
+      for (int h = 0; h < H; ++h)
+        if (ok[h]) row_store(to[h], left, v[h]);
+    }
+  };
+  float(&all)[H * 8] = reinterpret_cast<float(&)[H * 8]>(v);
+  if (e.z_out) store(z_out);
+  if (!e.z_in) activate<sizeof(O) == 2>(all, e.act);
+  if (e.d.rng) {
+#pragma unroll
+    for (int h = 0; h < H; ++h) dropout8(word[h], e.d.thr, e.d.scale, v[h]);
+  }
+  if (e.z_in || e.res) {
+    float s[H][8];
+#pragma unroll
+    for (int h = 0; h < H; ++h) widen(side[h], s[h]);
+    float(&flat)[H * 8] = reinterpret_cast<float(&)[H * 8]>(s);
+    if (e.z_in) {
+      times_slope(all, flat, e.act);
+    } else {
+#pragma unroll
+      for (int k = 0; k < H * 8; ++k) all[k] += flat[k];
     }
   }
-  row_store(out, left, v);
+  store(out);
 }
 template <typename O> __device__ inline const O *side_of(const Epilogue &e, long long &ld) {
   ld = e.z_in ? e.ldz : e.ldr;
@@ -495,7 +516,7 @@ __global__ __launch_bounds__(kThreads, WGS) void gemm_tile_kernel(TileArgs g) {
   const bool whole = g.splits == 1;
   const u64 base = g.e.d.rng && whole ? dropout_base(g.e.d.rng) : 0;
   constexpr int LPR = WTN / 8, RPP = 64 / LPR, PASSES = 32 / RPP;   // lanes a row, rows a pass, passes of 32 rows
-  static_assert(!AR || sizeof(Raw8<O>) * PASSES * 64 <= (size_t)kSide, "LDS");
+  static_assert(PASSES % 2 == 0 && (!AR || sizeof(Raw8<O>) * PASSES * 64 <= (size_t)kSide), "passes");
   char *const mine = lds + wave * (32 * kPitch + kSide);
   Raw8<O> *const mine_side = reinterpret_cast<Raw8<O> *>(mine + 32 * kPitch) + lane;   // a lane's own
   const int c = (lane % LPR) * 8, j = j0 + wn * WTN + c, left = g.J - j;
@@ -516,21 +537,26 @@ __global__ __launch_bounds__(kThreads, WGS) void gemm_tile_kernel(TileArgs g) {
     __builtin_amdgcn_wave_barrier();
   };
   f32x4 v0, v1;
-  Raw8<O> vs;
   auto get = [&](int p) {   // pass p of the 32 rows
     const char *at = mine + (p * RPP + lane / LPR) * kPitch + c * 4;
     v0 = *reinterpret_cast<const f32x4 *>(at);
     v1 = *reinterpret_cast<const f32x4 *>(at + 16);
   };
   if (j0 + BN > g.J || (whole && (g.e.act != RESIST_ACT_NONE || g.e.d.rng || g.e.z_out || g.e.res || g.e.z_in))) {
+    // Addresses are a base for the wave, which goes on from pass to pass, and a lane's part, which does not
     long long ld_side;
-    const O *side = side_of<O>(g.e, ld_side);
-    side += row0 * ld_side + j;
+    const O *side0 = side_of<O>(g.e, ld_side);
+    const long long wrow = i0 + wm * WTM, wcol = j0 + wn * WTN;
+    const int lrow = lane / LPR;
+    const char *side = reinterpret_cast<const char *>(side0 + wrow * ld_side + wcol);
+    const unsigned vside = (unsigned)((lrow * ld_side + c) * sizeof(O)), vout = (unsigned)((lrow * g.e.ldo + c) * sizeof(O)), vz = (unsigned)((lrow * g.e.ldz + c) * sizeof(O)),
+                   vpart = (unsigned)(((long long)lrow * g.J + c) * 4);
+    char *out = reinterpret_cast<char *>(static_cast<O *>(g.e.out) + wrow * g.e.ldo + wcol), *z_out = reinterpret_cast<char *>(static_cast<O *>(g.e.z_out) + wrow * g.e.ldz + wcol),
+         *part = reinterpret_cast<char *>(g.part + ((long long)split * g.I + wrow) * g.J + wcol);
+    u64 word = base + ((u64)row0 * (unsigned)g.e.words + (unsigned)(j >> 1)) * kGolden;
+    const u64 word_step = (u64)(RPP * (unsigned)g.e.words) * kGolden;
     constexpr bool kSided = AR;   // a weight gradient has nothing beside it
     const bool has_side = kSided && whole && (g.e.z_in || g.e.res), early = has_side && j0 + BN <= g.J;
-    O *out = static_cast<O *>(g.e.out) + row0 * g.e.ldo + j, *z_out = static_cast<O *>(g.e.z_out) + row0 * g.e.ldz + j;
-    float *part = g.part + ((long long)split * g.I + row0) * g.J + j;
-    u64 word = (u64)row0 * (unsigned)g.e.words + (unsigned)(j >> 1);
     float bias[8] = {};
     if (whole) bias_of(g.e, j, left, bias);
     Raw8<O> ahead[kSided ? TM : 1][PASSES];
@@ -540,7 +566,7 @@ __global__ __launch_bounds__(kThreads, WGS) void gemm_tile_kernel(TileArgs g) {
 #pragma unroll
         for (int p = 0; p < PASSES; ++p) {
           const int r = (k * PASSES + p) * RPP;
-          raw_load(side + (r < rows ? r : 0) * ld_side - (rows > 0 ? 0 : row0 * ld_side), 8, ahead[kSided ? k : 0][p]);   // of a row that is there, whichever
+          raw_load(side0 + (rows > 0 ? row0 + (r < rows ? r : 0) : 0) * ld_side + j, 8, ahead[kSided ? k : 0][p]);   // of a row that is there, whichever
         }
     }
     auto bring = [&](auto kc) {
@@ -558,25 +584,38 @@ __global__ __launch_bounds__(kThreads, WGS) void gemm_tile_kernel(TileArgs g) {
       if (TM > 2 && k == 2) bring(std::integral_constant<int, TM - 1 < 2 ? TM - 1 : 2>{});
       if (TM > 3 && k == 3) bring(std::integral_constant<int, TM - 1 < 3 ? TM - 1 : 3>{});
       meet_lanes();
-      get(0);
 #pragma unroll 1
-      for (int p = 0; p < PASSES; ++p, at += RPP) {
-        float v[8] = {v0[0], v0[1], v0[2], v0[3], v1[0], v1[1], v1[2], v1[3]};
-        get(p + 1 < PASSES ? p + 1 : p);
-        if (at < rows) {
-          if (whole) {
-            if (early) vs = mine_side[p * 64];
-            else if (has_side) raw_load(side, left, vs);
-            finish8<O>(g.e, out, z_out, word, left, v, bias, vs, base);
-          } else {
-            row_store(part, left, v);
-          }
+      for (int p = 0; p < PASSES; p += 2, at += 2 * RPP) {
+        float v[2][8];
+        Raw8<O> vs[2] = {};
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          get(p + h);
+#pragma unroll
+          for (int e = 0; e < 4; ++e) { v[h][e] = v0[e]; v[h][e + 4] = v1[e]; }
+          if (early) vs[h] = mine_side[(p + h) * 64];
         }
-        side += RPP * ld_side;
-        part += (long long)RPP * g.J;
-        out += RPP * g.e.ldo;
-        z_out += RPP * g.e.ldz;
-        word += RPP * (unsigned)g.e.words;
+        const bool ok[2] = {at < rows, at + RPP < rows};
+        if (whole) {
+          if (has_side && !early) {
+#pragma unroll
+            for (int h = 0; h < 2; ++h)
+              if (ok[h]) raw_load(reinterpret_cast<const O *>(side + h * RPP * ld_side * (int)sizeof(O) + vside), left, vs[h]);
+          }
+          O *const outs[2] = {reinterpret_cast<O *>(out + vout), reinterpret_cast<O *>(out + RPP * g.e.ldo * (int)sizeof(O) + vout)};
+          O *const zs[2] = {reinterpret_cast<O *>(z_out + vz), reinterpret_cast<O *>(z_out + RPP * g.e.ldz * (int)sizeof(O) + vz)};
+          const u64 words[2] = {word, word + word_step};
+          finish_rows<O, 2>(g.e, outs, zs, words, left, ok, v, bias, vs);
+        } else {
+#pragma unroll
+          for (int h = 0; h < 2; ++h)
+            if (ok[h]) row_store(reinterpret_cast<float *>(part + h * (long long)RPP * g.J * 4 + vpart), left, v[h]);
+        }
+        side += 2 * RPP * ld_side * (int)sizeof(O);
+        part += 2 * (long long)RPP * g.J * 4;
+        out += 2 * RPP * g.e.ldo * (int)sizeof(O);
+        z_out += 2 * RPP * g.e.ldz * (int)sizeof(O);
+        word += 2 * word_step;
       }
       meet_lanes();
     }
@@ -643,18 +682,20 @@ __global__ __launch_bounds__(kThreads) void gemm_join_kernel(JoinArgs a) {
   bias_of(a.e, j, left, bias);
   long long ld;
   const O *side = side_of<O>(a.e, ld);
-  Raw8<O> now = {};
-  if (side) raw_load(side + row * ld + j, left, now);
-  float v[8];
-  row_load(a.part + row * a.J + j, left, v);
+  Raw8<O> now[1] = {};
+  if (side) raw_load(side + row * ld + j, left, now[0]);
+  float v[1][8];
+  row_load(a.part + row * a.J + j, left, v[0]);
   for (int s = 1; s < a.splits; ++s) {
     float w[8];
     row_load(a.part + ((long long)s * a.I + row) * a.J + j, left, w);
 #pragma unroll
-    for (int k = 0; k < 8; ++k) v[k] += w[k];
+    for (int k = 0; k < 8; ++k) v[0][k] += w[k];
   }
-  finish8<O>(a.e, static_cast<O *>(a.e.out) + row * a.e.ldo + j, static_cast<O *>(a.e.z_out) + row * a.e.ldz + j, (u64)row * (unsigned)a.e.words + (unsigned)(j >> 1), left, v, bias, now,
-             a.e.d.rng ? dropout_base(a.e.d.rng) : 0);
+  O *const out[1] = {static_cast<O *>(a.e.out) + row * a.e.ldo + j}, *const z_out[1] = {static_cast<O *>(a.e.z_out) + row * a.e.ldz + j};
+  const u64 word[1] = {a.e.d.rng ? dropout_base(a.e.d.rng) + ((u64)row * (unsigned)a.e.words + (unsigned)(j >> 1)) * kGolden : 0};
+  const bool ok[1] = {true};
+  finish_rows<O, 1>(a.e, out, z_out, word, left, ok, v, bias, now);
 }
 
 // ---- few rows -------------------------------------------------------------------------------------------------------
