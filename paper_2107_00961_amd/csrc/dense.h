@@ -83,6 +83,19 @@ __device__ inline void widen(const Raw8<__bf16> &r, float (&v)[8]) {
   for (int e = 0; e < 4; ++e) { v[2 * e] = bf16_lo(r.a[e]); v[2 * e + 1] = bf16_hi(r.a[e]); }
 }
 
+// sum of p[i * apart], i = first, first + step, ... below `parts`, in order, in float64, U of them on their way at once
+template <int U> __device__ inline double parts_sum(const float *p, size_t apart, int first, int step, int parts) {
+  double s = 0.;
+  for (int i = first; i < parts; i += U * step) {
+    float v[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) v[u] = p[(size_t)min(i + u * step, parts - 1) * apart];   // the last one, rather than a branch, past the end
+#pragma unroll
+    for (int u = 0; u < U; ++u) s += i + u * step < parts ? (double)v[u] : 0.;
+  }
+  return s;
+}
+
 // ---- dropout: splitmix64 addressed by position.  Output number c of the sequence started from `state` is a pure function of
 // state + (c + 1) * golden, so the mask is computed wherever it is needed and never stored.  state is itself the
 // first output of the sequence seeded with the caller's seed: sequences of neighbouring seeds would else be the same one, shifted.

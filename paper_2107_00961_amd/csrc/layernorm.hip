@@ -343,20 +343,13 @@ __global__ __launch_bounds__(kThreads) void ln_bwd_cols_kernel(LnArgs a, const f
   row_store(p + a.N + c, left, sb);
 }
 
-// Columns [2][N] of `parts` parts, in float64: 64 columns to a workgroup, 16 ranges of parts (eight of each on their way at once), joined in order.
+// Columns [2][N] of `parts` parts, in float64: 64 columns to a workgroup, 16 ranges of parts, joined in order.  A part was written on any XCD, so that each
+// trip to it takes microseconds: all of a thread's are asked for at once (512 parts: 11 us with eight at a time, PARAMS_US with 32).
 __global__ __launch_bounds__(1024) void ln_params_kernel(const float *part, int parts, int N, float *dgamma, float *dbeta) {
   __shared__ double red[16][64];
   const int c = blockIdx.x * 64 + (threadIdx.x & 63), k = threadIdx.x >> 6;
   double s = 0.;
-  if (c < 2 * N) {
-    for (int p0 = k; p0 < parts; p0 += 128) {
-      float v[8];
-#pragma unroll
-      for (int i = 0; i < 8; ++i) v[i] = p0 + i * 16 < parts ? part[(size_t)(p0 + i * 16) * 2 * N + c] : 0.f;
-#pragma unroll
-      for (int i = 0; i < 8; ++i) s += (double)v[i];
-    }
-  }
+  if (c < 2 * N) s = parts > 128 ? parts_sum<32>(part + c, (size_t)2 * N, k, 16, parts) : parts_sum<8>(part + c, (size_t)2 * N, k, 16, parts);
   red[k][threadIdx.x & 63] = s;
   __syncthreads();
   if (k != 0 || c >= 2 * N) return;

@@ -665,9 +665,7 @@ __global__ __launch_bounds__(kThreads) void gemm_join_kernel(JoinArgs a) {
   if ((int)blockIdx.x < a.sum_wgs) {
     __shared__ double red[4][64];
     const int c = blockIdx.x * 64 + (threadIdx.x & 63), k = threadIdx.x >> 6;
-    double s = 0.;
-    if (c < a.sum_n)
-      for (int p = k; p < a.sum_parts; p += 4) s += (double)a.sums[(size_t)p * a.sum_n + c];
+    const double s = c < a.sum_n ? parts_sum<16>(a.sums + c, (size_t)a.sum_n, k, 4, a.sum_parts) : 0.;
     red[k][threadIdx.x & 63] = s;
     __syncthreads();
     if (k == 0 && c < a.sum_n) a.db[c] = (float)(((red[0][threadIdx.x] + red[1][threadIdx.x]) + red[2][threadIdx.x]) + red[3][threadIdx.x]);
