@@ -137,12 +137,13 @@ constexpr float kGeluC = 0.7978845608028654f, kGeluK = 0.044715f, kInvSqrt2Pi = 
 __device__ inline float exp2_f(float x) { return __builtin_amdgcn_exp2f(x); }   // one instruction each, within a step
 __device__ inline float rcp_f(float x) { return __builtin_amdgcn_rcpf(x); }
 __device__ inline float sigmoid_f(float x) { return rcp_f(1.f + exp2_f(-kLog2e * x)); }
-// Far out, where Phi and the derivatives are 0 or 1 to the last bit, an argument is held back: its own growth would meet that zero as infinity.
-__device__ inline float held(float z, float most) { return z > most ? most : z < -most ? -most : z; }   // a NaN stays one
+// Far out, where Phi and the derivatives are 0 or 1 to the last bit, what grows is held back: it would meet that zero as infinity.  (One
+// instruction; of a NaN it makes a number, but the other factor is one as well then.)
+__device__ inline float held(float z, float most) { return __builtin_amdgcn_fmed3f(z, -most, most); }
 // Q(x) = 1 - Phi(x) for 0 <= x <= 20, and e = exp(-x^2/2), which is phi(x) sqrt(2 pi).  Q(x)/e, Mills' ratio over sqrt(2 pi), is nearly a
 // polynomial in t = 1/(1 + c x): this one (of degree 8 without a constant, fitted to the least relative error on 0 ... 14.5, with c) is
-// off by 1e-7 of itself, x Q(x) in fp32 by 8e-8 at most.  Half the instructions of erfcf.
-__device__ inline float upper_tail(float x, float &e) {
+// off by 1e-7 of itself, x Q(x) in fp32 by 8e-8 at most.  Half the instructions of erfcf.  -> Q(x)/e
+__device__ inline float upper_tail_over(float x, float &e) {
   const float t = rcp_f(__builtin_fmaf(0.3050354009f, x, 1.f));
   float p = 0.03664687152f;
   p = __builtin_fmaf(p, t, -0.1527197052f);
@@ -153,10 +154,10 @@ __device__ inline float upper_tail(float x, float &e) {
   p = __builtin_fmaf(p, t, 0.1224711978f);
   p = __builtin_fmaf(p, t, 0.1216544519f);
   e = exp2_f(x * x * (-0.5f * kLog2e));
-  return p * t * e;
+  return p * t;
 }
 // Phi(z) to 3e-5 of itself for |z| < 3, and z Phi(z) to 1e-6 beyond: the logistic of an odd polynomial of degree 9 (fitted to log Phi(z)/Phi(-z)
-// with that allowance), for results that are rounded to bf16 (2^-9 of themselves).  Half the instructions of upper_tail.
+// with that allowance), for results that are rounded to bf16 (2^-9 of themselves).  Half the instructions of upper_tail_over.
 __device__ inline float phi_coarse(float z) {
   const float q = z * z;
   float p = 2.0995009433e-06f;
@@ -179,7 +180,8 @@ template <bool COARSE, int V> __device__ inline void activate(float (&v)[V], int
       } else {
         const float z = v[k], x = fabsf(z) > 20.f ? 20.f : fabsf(z);
         float e;
-        v[k] = (z > 0.f ? z : 0.f) - x * upper_tail(x, e);
+        const float q = upper_tail_over(x, e);
+        v[k] = (z > 0.f ? z : 0.f) - x * q * e;
       }
     }
   } else if (act == RESIST_ACT_GELU_TANH) {
@@ -198,22 +200,23 @@ template <int V> __device__ inline void times_slope(float (&v)[V], const float (
   } else if (act == RESIST_ACT_GELU) {
 #pragma unroll
     for (int k = 0; k < V; ++k) {
-      const float t = held(z[k], 20.f);
+      // at x = |z|, Phi(-x) - x phi(x) = (Q/e - x/sqrt(2 pi)) e is a'(-x), and 1 - a'(x)
+      const float x = fabsf(z[k]);
       float e;
-      const float q = upper_tail(fabsf(t), e);
-      v[k] *= __builtin_fmaf(t * kInvSqrt2Pi, e, t > 0.f ? 1.f - q : q);
+      const float q = upper_tail_over(x, e), r = e * __builtin_fmaf(-kInvSqrt2Pi, held(x, 20.f), q);
+      v[k] *= z[k] > 0.f ? 1.f - r : r;
     }
   } else if (act == RESIST_ACT_GELU_TANH) {
 #pragma unroll
     for (int k = 0; k < V; ++k) {
-      const float t = held(z[k], 20.f), s = sigmoid_f(2.f * kGeluC * (t + kGeluK * t * t * t));
-      v[k] *= s + t * s * (1.f - s) * 2.f * kGeluC * (1.f + 3.f * kGeluK * t * t);
+      const float s = sigmoid_f(2.f * kGeluC * (z[k] + kGeluK * z[k] * z[k] * z[k])), t = held(z[k], 20.f);
+      v[k] *= s + s * (1.f - s) * t * (2.f * kGeluC + 6.f * kGeluC * kGeluK * t * t);
     }
   } else if (act == RESIST_ACT_SILU) {
 #pragma unroll
     for (int k = 0; k < V; ++k) {
-      const float t = held(z[k], 200.f), s = sigmoid_f(t);
-      v[k] *= s + t * s * (1.f - s);
+      const float s = sigmoid_f(z[k]);
+      v[k] *= s + s * (1.f - s) * held(z[k], 200.f);
     }
   }
 }

@@ -199,6 +199,15 @@ def test_gradient_through_dropout_and_activation(act, dt):
 
 
 @pytest.mark.parametrize("dt", ["f32", "bf16"])
+@pytest.mark.parametrize("act", ACTS[1:])
+def test_gradient_where_z_is_not_finite(act, dt):
+    z = torch.tensor([[np.inf, -np.inf, np.nan] * 5], device="cuda").to(DT[dt])
+    got = R.dropout_backward(torch.full_like(z, 3.0), 0.0, None, act=act, z=z).float().reshape(5, 3)
+    assert (got[:, 0] == 3).all() and (got[:, 1] == 0).all()
+    assert (got[:, 2] == 0).all() if act == "relu" else torch.isnan(got[:, 2]).all()
+
+
+@pytest.mark.parametrize("dt", ["f32", "bf16"])
 @pytest.mark.parametrize("act", ACTS)
 def test_activation_of_a_dense_layer(act, dt):
     """w = 1: the product is x itself, so this is the activation over its range, and z comes back unchanged."""
