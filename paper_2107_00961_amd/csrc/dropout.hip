@@ -1,7 +1,8 @@
 // Dropout whose mask is a function of {seed, offset} and position (dense.h), so that nothing but the tensor itself is read or stored:
 //   forward   y  = [residual +] kept ? x / (1 - p) : 0
 //   backward  dx = a'(z) * (kept ? dy / (1 - p) : 0)      a: the activation in front of the dropout, z: what it was applied to
-// A thread takes eight consecutive elements of a row: four words of the sequence.
+// A thread takes eight consecutive elements of a row: four words of the sequence, which are two 64-bit products each.  Bound by memory: 16384 x 4096
+// bf16 51 us, with a residual 74 ... 77 (5.2 TB/s), fp32 137 (5.9); in bf16 through GELU's gradient, where the arithmetic shows, 91 us (4.4 TB/s).
 #include <algorithm>
 
 #include "conv_tile.h"

@@ -50,7 +50,7 @@ template <int LANES> __device__ inline float lanes_sum(float v) {
   }
   return v;
 }
-// The sums over the TPR threads of a row.  red: [2][waves of the workgroup], where a row is a workgroup's; `turn` alternates from call to call, so
+// The sums over the TPR threads of a row.  red: [2][waves of the workgroup], where a row is more than a wave's; `turn` alternates from call to call, so
 // that one barrier is enough: who writes a turn's words has met everyone since they were read.
 template <int TPR> __device__ inline void row_sums(float &a, float &b, float2 (*red)[8], int turn) {
   a = lanes_sum<(TPR < 64 ? TPR : 64)>(a);
@@ -61,7 +61,7 @@ template <int TPR> __device__ inline void row_sums(float &a, float &b, float2 (*
     a = b = 0.f;
 #pragma unroll
     for (int w = 0; w < TPR / 64; ++w) {
-      const float2 t = red[turn][w];
+      const float2 t = red[turn][threadIdx.x / TPR * (TPR / 64) + w];
       a += t.x;
       b += t.y;
     }
@@ -73,7 +73,17 @@ template <int TPR> __device__ inline float row_sum(float v, float2 (*red)[8], in
   return v;
 }
 
-// TPR threads a row, NV vectors of eight each
+// Where a thread's eight elements from column c on are taken from: the last vector of a row ends with the row, so that all of them are whole (of rows of
+// eight or more), and its first `skip` elements are another thread's too, who counts them (both store the same).  All eight are skipped past the row's
+// end.  16384 x 1100 bf16, with the last vector's elements one by one: forward 26 us, backward 54; so 23 and 39.
+struct Place {
+  int c, skip, count;
+  __device__ inline Place(int at, int N) : c(min(at, max(N - 8, 0))), skip(at - c), count(min(N, 8)) {}
+  __device__ inline bool counts(int e) const { return (unsigned)(e - skip) < (unsigned)count; }
+};
+
+// TPR threads a row, NV vectors of eight each.  Bound by memory: 16384 x 4096 bf16 46 us (5.8 TB/s; a copy of 1 GiB reaches 5.1), fp32 109 us (4.9),
+// 5003 x 1001 fp32, whose rows start anywhere, 9.8 us (4.1); one row of 4096 3.3 us, a launch.
 template <typename T, int TPR, int NV>
 __global__ __launch_bounds__(threads_of(TPR)) void ln_fwd_kernel(LnArgs a) {
   __shared__ float2 red[2][8];
@@ -86,21 +96,26 @@ __global__ __launch_bounds__(threads_of(TPR)) void ln_fwd_kernel(LnArgs a) {
   float s = 0.f;
 #pragma unroll
   for (int i = 0; i < NV; ++i) {
-    const int c = (t + i * TPR) * 8;
-    row_load(x + c, a.N - c, v[i]);
+    const Place p((t + i * TPR) * 8, a.N);
+    row_load(x + p.c, a.N - p.c, v[i]);
   }
 #pragma unroll
-  for (int i = 0; i < NV; ++i) s += ((v[i][0] + v[i][1]) + (v[i][2] + v[i][3])) + ((v[i][4] + v[i][5]) + (v[i][6] + v[i][7]));
+  for (int i = 0; i < NV; ++i) {
+    const Place p((t + i * TPR) * 8, a.N);
+    float m[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) m[e] = p.counts(e) ? v[i][e] : 0.f;
+    s += ((m[0] + m[1]) + (m[2] + m[3])) + ((m[4] + m[5]) + (m[6] + m[7]));
+  }
   const float mu = row_sum<TPR>(s, red, 0) / (float)a.N;
   float q = 0.f;
 #pragma unroll
   for (int i = 0; i < NV; ++i) {
-    const int c = (t + i * TPR) * 8;
+    const Place p((t + i * TPR) * 8, a.N);
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
-      const float d = c + e < a.N ? v[i][e] - mu : 0.f;
-      v[i][e] = d;
-      q += d * d;
+      v[i][e] -= mu;
+      q += p.counts(e) ? v[i][e] * v[i][e] : 0.f;
     }
   }
   const float r = 1.f / sqrtf(row_sum<TPR>(q, red, 1) / (float)a.N + a.eps);
@@ -108,11 +123,12 @@ __global__ __launch_bounds__(threads_of(TPR)) void ln_fwd_kernel(LnArgs a) {
   T *y = static_cast<T *>(a.out) + row * a.ldo;
 #pragma unroll
   for (int i = 0; i < NV; ++i) {
-    const int c = (t + i * TPR) * 8, left = a.N - c;
-    if (left <= 0) break;
+    const Place p((t + i * TPR) * 8, a.N);
+    const int left = a.N - p.c;
+    if (p.skip >= 8) break;
     float g[8], b[8];
-    if (a.gamma) row_load(a.gamma + c, left, g);
-    if (a.beta) row_load(a.beta + c, left, b);
+    if (a.gamma) row_load(a.gamma + p.c, left, g);
+    if (a.beta) row_load(a.beta + p.c, left, b);
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
       float o = v[i][e] * r;
@@ -120,7 +136,7 @@ __global__ __launch_bounds__(threads_of(TPR)) void ln_fwd_kernel(LnArgs a) {
       if (a.beta) o += b[e];
       v[i][e] = o;
     }
-    row_store(y + c, left, v[i]);
+    row_store(y + p.c, left, v[i]);
   }
   if (t == 0) {
     if (a.mean) a.mean[row] = mu;
@@ -128,7 +144,7 @@ __global__ __launch_bounds__(threads_of(TPR)) void ln_fwd_kernel(LnArgs a) {
   }
 }
 
-// rows that do not fit: a workgroup reads each three times (the second and third from L2)
+// rows that do not fit: a workgroup reads each three times (the second and third from a cache).  4096 x 16384 bf16 77 us (3.5 TB/s of what is read once)
 template <typename T>
 __global__ __launch_bounds__(kThreads) void ln_fwd_long_kernel(LnArgs a) {
   __shared__ float2 red[2][8];
@@ -174,7 +190,9 @@ __global__ __launch_bounds__(kThreads) void ln_fwd_long_kernel(LnArgs a) {
 }
 
 // A workgroup takes rows blockIdx.x, + gridDim.x, ... (a row per TPR threads): its threads keep their columns, so dy xhat and dy are summed
-// over its rows in registers.  The threads of other rows add theirs through LDS at the end.
+// over its rows in registers.  The threads of other rows add theirs through LDS at the end.  Bound by memory, of few rows by the trips to it, a
+// row's for each turn.  With ln_params_kernel, 16384 x 4096 bf16 88 ... 98 us whether or not with an
+// addend (5.5 TB/s with), 16384 x 2048 43 us, 16384 x 1024 27, 777 x 513 fp32 9.9.
 template <typename T, int TPR, int NV>
 __global__ __launch_bounds__(threads_of(TPR)) void ln_bwd_kernel(LnArgs a) {
   constexpr int RPW = threads_of(TPR) / TPR;
@@ -195,22 +213,23 @@ __global__ __launch_bounds__(threads_of(TPR)) void ln_bwd_kernel(LnArgs a) {
     const T *x = static_cast<const T *>(a.x) + rr * a.ldx, *dy = static_cast<const T *>(a.dy) + rr * a.lddy, *ad = static_cast<const T *>(a.addend) + rr * a.lda;
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
-      const int c = (t + i * TPR) * 8, left = live ? a.N - c : 0;
+      const int c = Place((t + i * TPR) * 8, a.N).c, left = live ? a.N - c : 0;
       raw_load(x + c, left, rx[i]);
       raw_load(dy + c, left, rdy[i]);
       if (a.addend) raw_load(ad + c, left, rad[i]);
     }
-    mu = a.mean[rr];
-    r = a.rstd[rr];
+    mu = live ? a.mean[rr] : 0.f;
+    r = live ? a.rstd[rr] : 0.f;
   };
   float w[NV][8];
 #pragma unroll
   for (int i = 0; i < NV; ++i) {
-    const int c = (t + i * TPR) * 8;
+    const int c = Place((t + i * TPR) * 8, a.N).c;
 #pragma unroll
     for (int e = 0; e < 8; ++e) w[i][e] = 1.f;
     if (a.gamma) row_load(a.gamma + c, a.N - c, w[i]);
   }
+  const bool full = a.N == TPR * NV * 8;   // no thread without elements, or with another's: 16384 x 4096 in bf16 99 -> 88 us
   int turn = 0;
   ask((long long)blockIdx.x * RPW + sub);
   for (long long row0 = (long long)blockIdx.x * RPW; row0 < a.M; row0 += step) {
@@ -219,22 +238,27 @@ __global__ __launch_bounds__(threads_of(TPR)) void ln_bwd_kernel(LnArgs a) {
     const float rs = r;
     float g[NV][8], h[NV][8], s1 = 0.f, s2 = 0.f;
     Raw8<T> add[NV];
+    auto terms = [&](auto masked) {
 #pragma unroll
-    for (int i = 0; i < NV; ++i) {
-      const int c = (t + i * TPR) * 8, left = live ? a.N - c : 0;
-      widen(rx[i], h[i]);
-      widen(rdy[i], g[i]);
-      add[i] = rad[i];
+      for (int i = 0; i < NV; ++i) {
+        const Place p((t + i * TPR) * 8, a.N);
+        widen(rx[i], h[i]);
+        widen(rdy[i], g[i]);
+        add[i] = rad[i];
 #pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        h[i][e] = e < left ? (h[i][e] - mu) * rs : 0.f;
-        sg[i][e] += g[i][e] * h[i][e];
-        sb[i][e] += g[i][e];
-        g[i][e] *= w[i][e];
-        s1 += g[i][e];
-        s2 += g[i][e] * h[i][e];
+        for (int e = 0; e < 8; ++e) {
+          h[i][e] = (h[i][e] - mu) * rs;
+          sg[i][e] += g[i][e] * h[i][e];
+          sb[i][e] += g[i][e];
+          g[i][e] *= w[i][e];
+          const bool counts = !decltype(masked)::value || p.counts(e);
+          s1 += counts ? g[i][e] : 0.f;
+          s2 += counts ? g[i][e] * h[i][e] : 0.f;
+        }
       }
-    }
+    };
+    if (full) terms(std::false_type{});
+    else terms(std::true_type{});
     ask(row + step);
     row_sums<TPR>(s1, s2, red, turn);
     turn ^= 1;
@@ -244,8 +268,8 @@ __global__ __launch_bounds__(threads_of(TPR)) void ln_bwd_kernel(LnArgs a) {
     T *dx = static_cast<T *>(a.out) + row * a.ldo;
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
-      const int c = (t + i * TPR) * 8, left = a.N - c;
-      if (left <= 0) break;
+      const Place p((t + i * TPR) * 8, a.N);
+      if (p.skip >= 8) break;
       float o[8];
       if (a.addend) widen(add[i], o);
 #pragma unroll
@@ -253,7 +277,7 @@ __global__ __launch_bounds__(threads_of(TPR)) void ln_bwd_kernel(LnArgs a) {
         const float d = rs * (g[i][e] - s1 - h[i][e] * s2);
         o[e] = a.addend ? o[e] + d : d;
       }
-      row_store(dx + c, left, o);
+      row_store(dx + p.c, a.N - p.c, o);
     }
   }
   if (!a.part) return;
@@ -278,17 +302,25 @@ __global__ __launch_bounds__(threads_of(TPR)) void ln_bwd_kernel(LnArgs a) {
     }
     if (sub != 0) return;
   }
-  float *p = a.part + (size_t)blockIdx.x * 2 * a.N;
+  float *part = a.part + (size_t)blockIdx.x * 2 * a.N;
 #pragma unroll
   for (int i = 0; i < NV; ++i) {
-    const int c = (t + i * TPR) * 8, left = a.N - c;
-    if (left <= 0) break;
-    row_store(p + c, left, sg[i]);
-    row_store(p + a.N + c, left, sb[i]);
+    const Place p((t + i * TPR) * 8, a.N);
+    if (p.skip == 0 && p.count == 8) {
+      row_store(part + p.c, 8, sg[i]);
+      row_store(part + a.N + p.c, 8, sb[i]);
+      continue;
+    }
+#pragma unroll
+    for (int e = 0; e < 8; ++e)
+      if (p.counts(e)) {
+        part[p.c + e] = sg[i][e];
+        part[a.N + p.c + e] = sb[i][e];
+      }
   }
 }
 
-// rows that do not fit: the sums of the rows first ...
+// rows that do not fit: the sums of the rows first (4096 x 16384 bf16, all three kernels, 158 us) ...
 template <typename T>
 __global__ __launch_bounds__(kThreads) void ln_bwd_rows_kernel(LnArgs a, float *sums) {
   __shared__ float2 red[2][8];
@@ -344,7 +376,8 @@ __global__ __launch_bounds__(kThreads) void ln_bwd_cols_kernel(LnArgs a, const f
 }
 
 // Columns [2][N] of `parts` parts, in float64: 64 columns to a workgroup, 16 ranges of parts, joined in order.  A part was written on any XCD, so that each
-// trip to it takes microseconds: all of a thread's are asked for at once (512 parts: 11 us with eight at a time, PARAMS_US with 32).
+// trip to it takes microseconds: all of a thread's are asked for at once (512 parts of 512 columns: 11 us
+// with eight at a time, 5 with 32; of 64 parts eight are 2.4 us, 32 with most of them past the end 5).
 __global__ __launch_bounds__(1024) void ln_params_kernel(const float *part, int parts, int N, float *dgamma, float *dbeta) {
   __shared__ double red[16][64];
   const int c = blockIdx.x * 64 + (threadIdx.x & 63), k = threadIdx.x >> 6;
@@ -359,20 +392,23 @@ __global__ __launch_bounds__(1024) void ln_params_kernel(const float *part, int 
   if (out) out[c < N ? c : c - N] = (float)s;
 }
 
-// Threads a row and vectors a thread: as few threads as hold a row in one or two vectors each, so that a wave takes several short rows at once.
+// Threads a row and vectors a thread: as few threads as hold a row in one or two vectors each, so that a wave or a workgroup takes several short rows at
+// once (16384 x 2048 bf16 in 128 threads or 256: forward 26 | 30 us, backward 43 | 50; in 64, four vectors each: 26 and 61).
 struct Held { int tpr, nv; };
 Held held_shape(int N) {
   if (N <= 128) return Held{16, 1};
   if (N <= 256) return Held{32, 1};
   if (N <= 512) return Held{64, 1};
   if (N <= 1024) return Held{64, 2};
-  if (N <= 2048) return Held{256, 1};
+  if (N <= 2048) return Held{128, 2};
   return N <= 4096 ? Held{256, 2} : Held{512, 2};
 }
 // Workgroups of the backward pass, each of which leaves a part of the columns' sums: two a CU (one where it is 512 threads) where there are rows enough for
 // two or more apiece (four where a part is long); with up to 64 rows (or groups of them) a row each, which is quicker than a second turn.
-// us, M x N, with 1 | 2 | 4 rows a turn:  777x513 fp32 12.0 | 11.7 | 13.6   2000x300 bf16 16.2 | 12.8 | 13.4   300x2000 bf16 13.9 | 11.2 | 11.7
-//   1000x4096 fp32 27.1 | 26.8 | 22.1   64x1024 fp32 7.8 | 8.7 | 10.8       16384x4096 bf16, 256 | 512 | 1024 workgroups 142 | 109 | 132
+// us, M x N, number of workgroups in brackets, the chosen one first:
+//   777x513 fp32 (98) 10.2, (192) 13.6, (64) 12.6     2000x300 bf16 (250) 11.0, (500) 10.3, (128) 11.6
+//   1000x4096 fp32 (250) 21.3, (500) 21.6, (1000) 28.2     4096x1024 bf16 (512) 14.4, (1024) 20.2, (256) 14.9     16384x4096 bf16 (512) 88, (1024) 100, (256) 134
+//   4096x8192 bf16 (256) 50, (512) 55, (192) 58     16384x2048 bf16 (512) 43, (256) 57, (1024) 48     4000x1100 bf16 (512) 21.5, (256) 27, (768) 23
 int bwd_parts(int64_t M, int N) {
   const Held h = held_shape(N);
   const int64_t rpw = N > kHeldCols ? 1 : threads_of(h.tpr) / h.tpr, turns = (M + rpw - 1) / rpw, each = N > 2048 ? 4 : 2;
@@ -387,7 +423,7 @@ int bwd_parts(int64_t M, int N) {
     else if (h.tpr == 32) call((kernel<T, 32, 1>), 32);                           \
     else if (h.tpr == 64 && h.nv == 1) call((kernel<T, 64, 1>), 64);              \
     else if (h.tpr == 64) call((kernel<T, 64, 2>), 64);                           \
-    else if (h.tpr == 256 && h.nv == 1) call((kernel<T, 256, 1>), 256);           \
+    else if (h.tpr == 128) call((kernel<T, 128, 2>), 128);                        \
     else if (h.tpr == 256) call((kernel<T, 256, 2>), 256);                        \
     else call((kernel<T, 512, 2>), 512);                                          \
   } while (0)

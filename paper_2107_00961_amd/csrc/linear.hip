@@ -5,7 +5,7 @@
 // All three are one product, out(i, j) = sum over r of a(i, r) b(j, r), with either index contiguous in either operand.  Products on the matrix
 // cores, sums in fp32, one rounding where a result is stored.  Three ways:
 //   tiles      (gemm_tile_kernel) bf16 operands, or the three bf16 parts of fp32 ones (conv3.hip says why that loses nothing)
-//   few rows   (few_rows_kernel) the forward pass of up to 16 rows: w is read once, straight into fragments
+//   few rows   (few_rows_*_kernel) w straight from memory into fragments, or dw straight from registers: bound by its bytes
 //   plain      (plain_tile) what of an fp32 product three parts do not hold, on the fp32 matrix instruction
 // Operands whose rows are not 16-byte aligned, and those in parts, are laid out in the workspace first (lay_out_kernel).
 #include <algorithm>
@@ -53,7 +53,7 @@ __device__ inline void finish(const Epilogue &e, long long i, int j, float v, u6
 // A matrix [rows][n] with `ld` elements between rows becomes [rows][to_ld] of bf16, to_ld a multiple of eight, with zeros behind a row's end:
 // a copy (bf16), or three planes of parts (fp32).  Parts whose rows are the reduction's axis lie [to_ld/32][rows][32], to_ld a multiple of 32: the
 // tiles read them 32 at a time, of which a row's 64 bytes would be half a line each.  Of parts, each 64x64 block also leaves a word: whether it has a value that three parts
-// do not hold (conv3.hip: not finite or rounding to infinity, or below 2^-110).
+// do not hold (conv3.hip: not finite or rounding to infinity, or below 2^-110).  2000 x 1024 and 1024 x 1024 in fp32, 31 MB in and out: 8 us.
 struct LayOut {
   const void *from;
   __bf16 *to;
@@ -128,7 +128,10 @@ __global__ __launch_bounds__(kThreads) void lay_out_kernel(LayOutArgs a) {
 // ---- tiles --------------------------------------------------------------------------------------------
 // Operand tiles go from memory straight into LDS (16 bytes a lane, 1 KB a wave and instruction, in lane order), STAGES deep, and from there
 // in fragments to the matrix cores.  Four waves, a quarter of the BM x BN tile each: the larger a wave's share, the fewer times a
-// staged element is read from LDS (256x256: 1024 clocks of reading and 512 of arriving for 2048 of products).
+// staged element is read from LDS (256x256: 1024 clocks of reading and 512 of arriving for 2048 of products).  Bound by the matrix cores and what
+// the chip's power leaves of its clock: 8192 x 8192 -> 2048 in bf16 201 us (1.37 PFLOP/s, the cores at work 66 % of the time; as weight gradient 214 us, 72 %),
+// 2000 x 1024 -> 1024 in fp32 30 us beside 8 of laying out.  The epilogue's arithmetic is not hidden, one workgroup having a compute unit to itself: through GELU and
+// dropout 8192 x 2048 -> 8192 takes 300 us for 227, and making the mask between the products, though it fits, 297.
 // Layout in LDS.  Lane order leaves no room for padding, so what keeps rows off each other's banks is which 16-byte piece a lane asks for:
 //   reduction contiguous (R): a row is an index i, BK values of r: piece c of row i lies at c ^ f(i), f = (i >> 1) & 7 (BK 64, two rows to 256
 //     bytes), (i >> 2) & 3 (BK 32, four rows): sixteen consecutive rows' pieces c fill the 256 bytes of the 64 banks;
@@ -914,9 +917,9 @@ __global__ __launch_bounds__(kThreads) void few_rows_wgrad_kernel(const T *dz, l
 
 // ---- plans ----------------------------------------------------------------------------------------------------------
 // Up to this many rows go without tiles.  us, 4096 -> 4096, tiles (with what they lay out and join) -> few rows:
-//   fp32 1 row: forward 52 -> 15, data gradient 53 -> 15, weight gradient 33 -> 13      17 rows: 53 -> 20, 55 -> 19, 34 -> as it was
-//   fp32 64 rows: 66 -> 38, 56 -> 40     bf16 1 row: forward 13 -> 7.1 (4.7 TB/s), data gradient 11 -> 40 (64 columns to a workgroup: tiles), weight gradient 27 -> 13 (5.2 TB/s)
-//   bf16 32 rows: forward 13.1 -> 13.7, at 512 -> 512 6.0 -> 3.9
+//   fp32 1 row: forward 50 -> 15, data gradient 54 -> 16, weight gradient 34 -> 13      17 rows: 50 -> 20, 55 -> 19, 34 (tiles)
+//   fp32 64 rows: 51 -> 39, 55 -> 40     bf16 1 row: forward 11.4 -> 7.4 (4.5 TB/s), data gradient 11.5 (tiles; 40 with 64 columns to a workgroup), weight gradient 27 -> 13.5 (5 TB/s)
+//   bf16 16 rows: forward 12.7 -> 10.1, weight gradient 27 -> 16     32 rows: forward 13.3 -> 14.1, at 512 -> 512 6.0 -> 4.5
 int few(int dt, int op) {
   if (op == 2) return 16;
   return dt == DT_F32 ? 64 : op == 0 ? 32 : 0;
@@ -941,9 +944,9 @@ FewPlan plan_few(int dt, int op, long long M, int J, int R) {
 // (`low` with a quarter of that many, `full` with all: the clock gives way under the products); a split reduction writes
 // its parts and reads them back in a launch of its own.  Either side of the choice, us measured, bf16 forward unless said
 // (M x K x N: 256x256 | 128x128 | 64x64):
-//   8192x8192x2048  212 | 261 | -       4096x2048x2048  54 | 38 | 61     512x4096x4096  89 | 49 | 30      64x512x512  16 | 8.3 | 5.6
-//   128x4096x512, 64x64: 1 split 21.4, 2 14.8, 4 11.2, 8 10.7            128x512x4096, 64x64: 1 split 5.7, 2 9.4, 4 11.5
-//   fp32 2048x1024x4096 (256x128 | 128x128 | 64x64)  100 | 108 | 146     fp32 2000x1024x1024  74 | 49 (2 splits 42) | 47
+//   8192x8192x2048  202 | 246 | 427     4096x2048x2048  47 | 38 | 60     512x4096x4096  77 | 43 | 31      64x512x512  16 | 8.1 | 6.1
+//   128x4096x512, 64x64: 1 split 22.2, 2 15.4, 4 11.8, 8 11.3            128x512x4096, 64x64: 1 split 6.4, 2 9.9, 4 12.0
+//   fp32 (256x128 | 128x128 | 64x64)  8192x2048x2048  324 | 335 | 383     2048x1024x4096  92 | 97 | 106     2000x1024x1024  63 | 45 (2 splits 40) | 36
 struct TileCost { int bm, bn, fit; double start, low, full; };
 constexpr int kSizes = 3;
 constexpr TileCost kTiles[2][kSizes] = {{{256, 256, 256, 7.0, 1.15, 1.58}, {128, 128, 512, 2.6, 0.58, 1.03}, {64, 64, 512, 1.4, 0.28, 0.42}},
