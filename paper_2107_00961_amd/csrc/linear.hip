@@ -287,9 +287,10 @@ __global__ __launch_bounds__(kThreads, WGS) void gemm_tile_kernel(TileArgs g) {
   constexpr int kLoadsA = NP * SA::kLoads, kLoads = kLoadsA + NP * SB::kLoads, kA = NP * SA::kBytes, kStage = kA + NP * SB::kBytes;
   constexpr int kPitch = WTN * 4 + 16, kSide = AR ? 32 * WTN * (int)sizeof(O) : 0, kOut = 4 * (32 * kPitch + kSide);
   static_assert(STAGES >= 2, "stages");
-  // Two stages only: a step's fragments are read in its first half, and what is staged next goes where they came from in the second half and the
-  // following step's first: transfers have two products of depth 16 or more to arrive in, and a stage less does.  (Fragments are
-  // read a product ahead else, and a stage is free a step later.  Waiting for transfers took 11 % of the 256x256 tile's time then.)
+  // Two stages only: a step's fragments are read in its first half, and what is staged next goes where they came from in the second half: transfers
+  // have four products of depth 16 to arrive in, and a stage less does.  (Fragments are read a product ahead else, and a stage is free a step later.
+  // Waiting for transfers took 11 % of the 256x256 tile's time then.  Spread over four products, the 128x128 tile of 4096 x 2048 x 2048 took 38 and, as
+  // weight gradient, 55 us for 37 and 49.)
   constexpr bool EARLY = STAGES == 2 && BK == 64 && NP == 1;
   constexpr int SETS = EARLY ? NK : 2;
   static_assert(TM <= 4, "tile");
@@ -302,13 +303,11 @@ __global__ __launch_bounds__(kThreads, WGS) void gemm_tile_kernel(TileArgs g) {
   const int j0 = tj * BN;
   const int steps = (int)((rend - rbeg + BK - 1) / BK);
 
-  // ---- operands to LDS.  left: bytes from the tile's current corner to the operand's end
+  // ---- operands to LDS
   constexpr bool PA = AR && NP == 3, PB = BR && NP == 3;   // in panels of 32 steps: [R/32][I][32]
   static_assert(NP == 1 || BK == 32, "panels");
   const char *pa = reinterpret_cast<const char *>(g.a + (PA ? (rbeg >> 5) * g.I * 32 + i0 * 32 : AR ? i0 * g.lda + rbeg : rbeg * g.lda + i0));
   const char *pb = reinterpret_cast<const char *>(g.b + (PB ? (rbeg >> 5) * g.J * 32 + (long long)j0 * 32 : BR ? (long long)j0 * g.ldb + rbeg : rbeg * g.ldb + j0));
-  long long left_a = PA ? (g.I - i0) * 64 : AR ? ((g.I - i0 - 1) * g.lda + (rend - rbeg + 7) / 8 * 8) * 2 : ((rend - rbeg - 1) * g.lda + (g.I - i0 + 7) / 8 * 8) * 2;
-  long long left_b = PB ? (long long)(g.J - j0) * 64 : BR ? ((g.J - j0 - 1) * g.ldb + (rend - rbeg + 7) / 8 * 8) * 2 : ((rend - rbeg - 1) * g.ldb + (g.J - j0 + 7) / 8 * 8) * 2;
   unsigned va[SA::kLoads], vb[SB::kLoads];
 #pragma unroll
   for (int p = 0; p < SA::kLoads; ++p) {
@@ -322,24 +321,43 @@ __global__ __launch_bounds__(kThreads, WGS) void gemm_tile_kernel(TileArgs g) {
   }
   // of a row of BK reduction steps: the first step of this lane's piece (the same in every instruction)
   const int ka = SA::piece(SA::row(0, wave, lane), lane) * 8, kb = SB::piece(SB::row(0, wave, lane), lane) * 8;
-  int left_r = (int)min(rend - rbeg, (long long)0x40000000);
+  int left_r = (int)(rend - rbeg);   // steps are rows of a matrix, or fewer
+  // Bytes of an operand from the tile's current corner on.  Where the reduction is contiguous, to the end of the last row: rows past it begin there or
+  // later at any step, and steps past the end are not asked for.  Else the rows that this step has, at most BK of them.
+  auto capped = [](long long n) { return (unsigned)min(n, 0x7ffffff0LL); };
+  unsigned size_a = PA ? capped((g.I - i0) * 64) : AR ? capped(((g.I - i0 - 1) * g.lda + (rend - rbeg + 7) / 8 * 8) * 2) : 0u;
+  unsigned size_b = PB ? capped((long long)(g.J - j0) * 64) : BR ? capped(((g.J - j0 - 1) * g.ldb + (rend - rbeg + 7) / 8 * 8) * 2) : 0u;
+  const unsigned row_a = (unsigned)g.lda * 2, row_b = (unsigned)g.ldb * 2, last_a = AR ? 0u : (unsigned)((g.I - i0 + 7) / 8 * 8) * 2, last_b = BR ? 0u : (unsigned)((g.J - j0 + 7) / 8 * 8) * 2;
+  auto measure = [&]() {
+    const int rows = min(left_r, BK);
+    if constexpr (!AR) size_a = rows > 0 ? (rows - 1) * row_a + last_a : 0u;
+    if constexpr (!BR) size_b = rows > 0 ? (rows - 1) * row_b + last_b : 0u;
+  };
+  measure();
   const unsigned lds_at = __builtin_amdgcn_readfirstlane((unsigned)(uintptr_t)(__attribute__((address_space(3))) char *)lds) + wave * 1024;
   auto request = [&](int p, int stage) {   // instruction p of the step
     const bool is_a = p < kLoadsA;
     const int q = is_a ? p : p - kLoadsA, per = is_a ? SA::kLoads : SB::kLoads, plane = q / per;
-    const __amdgpu_buffer_rsrc_t r = is_a ? make_rsrc(pa + plane * g.plane_a * 2, left_a > 0 ? (unsigned)min(left_a, 0x7ffffff0LL) : 0u)
-                                          : make_rsrc(pb + plane * g.plane_b * 2, left_b > 0 ? (unsigned)min(left_b, 0x7ffffff0LL) : 0u);
+    const __amdgpu_buffer_rsrc_t r = is_a ? make_rsrc(pa + plane * g.plane_a * 2, size_a) : make_rsrc(pb + plane * g.plane_b * 2, size_b);
     unsigned v = is_a ? va[q % per] : vb[q % per];
     if (is_a ? AR : BR) v = (is_a ? ka : kb) < left_r ? v : kOOB;
     transfer(r, v, lds_at + stage * kStage + (is_a ? 0 : kA) + q * 4096);
   };
-  auto advance = [&]() {
-    const long long da = PA ? g.I * 64 : (AR ? BK : BK * g.lda) * 2, db = PB ? g.J * 64LL : (BR ? BK : BK * g.ldb) * 2;
-    pa += da;
-    pb += db;
-    if constexpr (!PA) left_a -= da;   // (of panels, what is past the reduction's end is not asked for)
-    if constexpr (!PB) left_b -= db;
-    left_r -= BK;
+  const long long da = PA ? g.I * 64 : (AR ? BK : BK * g.lda) * 2, db = PB ? g.J * 64LL : (BR ? BK : BK * g.ldb) * 2;
+  // To the next step, in three pieces that fit beside a product each.  (Left alone, the compiler makes all of them at the loop's end, where nothing
+  // goes on beside them.)
+  auto advance = [&](int piece) {
+    if (piece == 0) {
+      pa += da;
+      asm volatile("" : "+s"(pa));
+    } else if (piece == 1) {
+      pb += db;
+      asm volatile("" : "+s"(pb));
+    } else {
+      left_r -= BK;
+      asm volatile("" : "+s"(left_r));
+      measure();
+    }
   };
 
   // ---- fragments from LDS: eight consecutive steps of the reduction of one index per lane, as they lie or by two transpose reads
@@ -392,14 +410,15 @@ __global__ __launch_bounds__(kThreads, WGS) void gemm_tile_kernel(TileArgs g) {
       for (int e = 0; e < 16; ++e) acc[i][j][e] = 0.f;
 
   // A step of the reduction asks for the tile STAGES steps ahead, whose place in LDS is free once all waves have met: an NK-th of its transfers with
-  // each of NK products of depth 16, from the last of the step before on (early: from the third).
+  // each of NK products of depth 16, from the last of the step before on (early: half with the third and half with the fourth).
   static_assert((STAGES - 1) * kLoads < 64, "transfers");
-  auto cut = [](int k) constexpr { return k * kLoads / NK; };   // a tile's transfers cut(k) .. cut(k + 1) go together
+  auto cut = [](int k) constexpr { return (EARLY && 2 * k < NK ? 2 * k : EARLY ? NK : k) * kLoads / NK; };   // a tile's transfers cut(k) .. cut(k + 1) go together
 #pragma unroll
   for (int s = 0; s < STAGES - 1; ++s) {
 #pragma unroll
     for (int p = 0; p < kLoads; ++p) request(p, s);
-    advance();
+#pragma unroll
+    for (int p = 0; p < 3; ++p) advance(p);
   }
   constexpr int kFirst = cut(EARLY ? 2 : 1);
 #pragma unroll
@@ -417,12 +436,12 @@ __global__ __launch_bounds__(kThreads, WGS) void gemm_tile_kernel(TileArgs g) {
     constexpr int k = decltype(kc)::value, PAIRS = NP == 3 ? 6 : 1, MF = PAIRS * TM * TN, MD = MF > 1 ? MF * 3 / 4 : 1, MH = EARLY || MF == 1 ? MF : MF / 2;
     constexpr bool last = k + 1 == NK;
     constexpr int set = EARLY ? k : k & 1;
-    if constexpr (EARLY && k == 2) {
-      advance();
-      meet();                                   // everyone has read this stage
-    }
+    if constexpr (EARLY && k == 2) meet();      // everyone has read this stage
     if constexpr (last) {
-      if constexpr (!EARLY) advance();
+      if constexpr (!EARLY) {
+#pragma unroll
+        for (int p = 0; p < 3; ++p) advance(p);
+      }
       wait_and_meet<EARLY ? cut(1) : (STAGES - 2) * kLoads>();   // the next stage is there
     }
     // fragments read beside these products: the next one's; early, of the 3 kFrags that are left of this step half with each of its first two
@@ -442,9 +461,11 @@ __global__ __launch_bounds__(kThreads, WGS) void gemm_tile_kernel(TileArgs g) {
         else if constexpr (EARLY) fetch(ds, 0, next, 0);
         else fetch(ds, (k + 1) & 1, last ? next : stage, last ? 0 : k + 1);
       }
+      if constexpr (EARLY && k == 1)
+        if (m + 3 >= MF) advance(m + 3 - MF);
 #pragma unroll
       for (; vm < (m + 1 < MH ? (m + 1) * VM / MH : VM); ++vm) {
-        if constexpr (EARLY) request(v0 + vm, k < 2 ? next : stage);
+        if constexpr (EARLY) request(v0 + vm, stage);
         else request(v0 + vm, last ? stage : refill);
       }
       __builtin_amdgcn_sched_barrier(0);
@@ -944,7 +965,7 @@ FewPlan plan_few(int dt, int op, long long M, int J, int R) {
 // (`low` with a quarter of that many, `full` with all: the clock gives way under the products); a split reduction writes
 // its parts and reads them back in a launch of its own.  Either side of the choice, us measured, bf16 forward unless said
 // (M x K x N: 256x256 | 128x128 | 64x64):
-//   8192x8192x2048  202 | 246 | 427     4096x2048x2048  47 | 38 | 60     512x4096x4096  77 | 43 | 31      64x512x512  16 | 8.1 | 6.1
+//   8192x8192x2048  202 | 246 | 427     4096x2048x2048  47 | 37 | 60     512x4096x4096  77 | 43 | 31      64x512x512  16 | 8.1 | 6.1
 //   128x4096x512, 64x64: 1 split 22.2, 2 15.4, 4 11.8, 8 11.3            128x512x4096, 64x64: 1 split 6.4, 2 9.9, 4 12.0
 //   fp32 (256x128 | 128x128 | 64x64)  8192x2048x2048  324 | 335 | 383     2048x1024x4096  92 | 97 | 106     2000x1024x1024  63 | 45 (2 splits 40) | 36
 struct TileCost { int bm, bn, fit; double start, low, full; };
