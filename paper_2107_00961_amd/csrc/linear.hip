@@ -129,7 +129,7 @@ __global__ __launch_bounds__(kThreads) void lay_out_kernel(LayOutArgs a) {
 // Operand tiles go from memory straight into LDS (16 bytes a lane, 1 KB a wave and instruction, in lane order), STAGES deep, and from there
 // in fragments to the matrix cores.  Four waves, a quarter of the BM x BN tile each: the larger a wave's share, the fewer times a
 // staged element is read from LDS (256x256: 1024 clocks of reading and 512 of arriving for 2048 of products).  Bound by the matrix cores and what
-// the chip's power leaves of its clock: 8192 x 8192 -> 2048 in bf16 201 us (1.37 PFLOP/s, the cores at work 66 % of the time; as weight gradient 214 us, 72 %),
+// the chip's power leaves of its clock: 8192 x 8192 -> 2048 in bf16 201 ... 210 us (1.35 PFLOP/s, the cores at work in 74 % of 357 thousand clocks at 1.7 GHz),
 // 2000 x 1024 -> 1024 in fp32 30 us beside 8 of laying out.  The epilogue's arithmetic is not hidden, one workgroup having a compute unit to itself: through GELU and
 // dropout 8192 x 2048 -> 8192 takes 300 us for 227, and making the mask between the products, though it fits, 297.
 // Layout in LDS.  Lane order leaves no room for padding, so what keeps rows off each other's banks is which 16-byte piece a lane asks for:
