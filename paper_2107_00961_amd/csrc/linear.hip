@@ -136,16 +136,18 @@ __global__ __launch_bounds__(kThreads) void lay_out_kernel(LayOutArgs a) {
 //   reduction contiguous (R): a row is an index i, BK values of r: piece c of row i lies at c ^ f(i), f = (i >> 1) & 7 (BK 64, two rows to 256
 //     bytes), (i >> 2) & 3 (BK 32, four rows): sixteen consecutive rows' pieces c fill the 256 bytes of the 64 banks;
 //   other index contiguous: a row is an r, BM values of i: piece c of row r lies at c ^ 4 (r & 3) (64 values, two rows to 256 bytes:
-//     c ^ 2 (r & 2)): the four rows of a transpose read, 64 bytes each, fill 256 bytes.
+//     c ^ 2 (r & 2)): the four rows of a transpose read, 64 bytes each, fill 256 bytes.  In fragments of 16 it has eight rows r, r + 1, .. r + 3, r + 8, ..
+//     of 32 bytes each: c ^ 2 (r & 3) ^ (r & 8).
 // Bounds: an operand's descriptor starts at the tile and ends with the operand (rows past it, and steps past it, come as zeros); its
 // contiguous axis is a multiple of eight where it is the reduction (a tail's pieces are not asked for) and may end in a piece where it is
 // not (what a tile has past its last column goes into outputs that are not stored).
 // Operands in three parts are three such tiles each, and a product is six (small ones first).
-template <bool R, int B, int BK> struct Stage {
+template <bool R, int B, int BK, int FR> struct Stage {
   static constexpr int kBytes = B * BK * 2, kLoads = kBytes / 4096;   // of a plane; a wave's instructions
   static constexpr int kRow = R ? BK * 2 : B * 2, kPieces = kRow / 16, kRows = 1024 / kRow;   // rows an instruction
   __device__ static inline int swizzle(int row) {
     if (R) return BK == 64 ? (row >> 1) & 7 : (row >> 2) & 3;
+    if (FR == 16) return (row & 3) << 1 | (row & 8);
     return kPieces == 8 ? (row & 2) << 1 : (row & 3) << 2;
   }
   // row and piece of the tile that lane `l` of wave `w` asks for with instruction p
@@ -233,6 +235,9 @@ template <int N> __device__ inline void wait_and_meet() {   // at most N of this
 
 __device__ inline void meet() { asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory"); }   // all reads done
 
+// f(0), f(1), ... as constants
+template <int... M, typename F> __device__ inline void each(std::integer_sequence<int, M...>, F f) { (f(std::integral_constant<int, M>{}), ...); }
+
 // the tile's place: `group` rows of tiles are walked column by column, an XCD's workgroups one after the other
 __device__ inline void tile_of(int bid, int tiles_i, int tiles_j, int group, int &ti, int &tj) {
   const int per = group * tiles_j, g = bid / per, rest = bid - g * per;
@@ -281,18 +286,20 @@ __device__ inline void plain_tile(const TileArgs &g, long long i0, int j0, long 
 
 template <typename O, bool AR, bool BR, int NP, int BM, int BN, int BK, int STAGES, int WGS>
 __global__ __launch_bounds__(kThreads, WGS) void gemm_tile_kernel(TileArgs g) {
-  using SA = Stage<AR, BM, BK>;
-  using SB = Stage<BR, BN, BK>;
-  constexpr int WTM = BM / 2, WTN = BN / 2, TM = WTM / 32, TN = WTN / 32, NK = BK / 16;
+  constexpr bool EARLY = STAGES == 2 && BK == 64 && NP == 1;
+  // Fragments of FR rows by FK of the reduction.  v_mfma_f32_16x16x32_bf16 moves less through the registers than 32x32x16 (a result is added to half as
+  // often), and the clock that the power limit leaves is what counts: 2.0 PFLOP/s with it alone, 1.8 with the other.
+  constexpr int FR = EARLY ? 16 : 32, FK = 512 / FR;
+  using SA = Stage<AR, BM, BK, FR>;
+  using SB = Stage<BR, BN, BK, FR>;
+  constexpr int WTM = BM / 2, WTN = BN / 2, TM = WTM / 32, FM = WTM / FR, FN = WTN / FR, NK = BK / FK;
   constexpr int kLoadsA = NP * SA::kLoads, kLoads = kLoadsA + NP * SB::kLoads, kA = NP * SA::kBytes, kStage = kA + NP * SB::kBytes;
   constexpr int kPitch = WTN * 4 + 16, kSide = AR ? 32 * WTN * (int)sizeof(O) : 0, kOut = 4 * (32 * kPitch + kSide);
   static_assert(STAGES >= 2, "stages");
-  // Two stages only: a step's fragments are read in its first half, and what is staged next goes where they came from in the second half: transfers
-  // have four products of depth 16 to arrive in, and a stage less does.  (Fragments are read a product ahead else, and a stage is free a step later.
-  // Waiting for transfers took 11 % of the 256x256 tile's time then.  Spread over four products, the 128x128 tile of 4096 x 2048 x 2048 took 38 and, as
+  // Two stages only (EARLY): a step's fragments are read in its first half, and what is staged next goes where they came from in the second half:
+  // transfers have half a step and more to arrive in, and a stage less does.  (Fragments are read a product ahead else, and a stage is free a step later.
+  // Waiting for transfers took 11 % of the 256x256 tile's time then.  Spread over all of a step, the 128x128 tile of 4096 x 2048 x 2048 took 38 and, as
   // weight gradient, 55 us for 37 and 49.)
-  constexpr bool EARLY = STAGES == 2 && BK == 64 && NP == 1;
-  constexpr int SETS = EARLY ? NK : 2;
   static_assert(TM <= 4, "tile");
   __shared__ __attribute__((aligned(1024))) char lds[STAGES * kStage > kOut ? STAGES * kStage : kOut];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), wm = wave >> 1, wn = wave & 1;
@@ -335,13 +342,23 @@ __global__ __launch_bounds__(kThreads, WGS) void gemm_tile_kernel(TileArgs g) {
   };
   measure();
   const unsigned lds_at = __builtin_amdgcn_readfirstlane((unsigned)(uintptr_t)(__attribute__((address_space(3))) char *)lds) + wave * 1024;
-  auto request = [&](int p, int stage) {   // instruction p of the step
+  auto aim = [&](int p, int stage, unsigned &v, unsigned &to) {   // of instruction p of the step: where from, where to
     const bool is_a = p < kLoadsA;
-    const int q = is_a ? p : p - kLoadsA, per = is_a ? SA::kLoads : SB::kLoads, plane = q / per;
-    const __amdgpu_buffer_rsrc_t r = is_a ? make_rsrc(pa + plane * g.plane_a * 2, size_a) : make_rsrc(pb + plane * g.plane_b * 2, size_b);
-    unsigned v = is_a ? va[q % per] : vb[q % per];
+    const int q = is_a ? p : p - kLoadsA, per = is_a ? SA::kLoads : SB::kLoads;
+    v = is_a ? va[q % per] : vb[q % per];
     if (is_a ? AR : BR) v = (is_a ? ka : kb) < left_r ? v : kOOB;
-    transfer(r, v, lds_at + stage * kStage + (is_a ? 0 : kA) + q * 4096);
+    to = lds_at + stage * kStage + (is_a ? 0 : kA) + q * 4096;
+    asm volatile("" : "+v"(v), "+s"(to));   // here, that is
+  };
+  auto go = [&](int p, unsigned v, unsigned to) {
+    const bool is_a = p < kLoadsA;
+    const int plane = is_a ? p / SA::kLoads : (p - kLoadsA) / SB::kLoads;
+    transfer(is_a ? make_rsrc(pa + plane * g.plane_a * 2, size_a) : make_rsrc(pb + plane * g.plane_b * 2, size_b), v, to);
+  };
+  auto request = [&](int p, int stage) {
+    unsigned v, to;
+    aim(p, stage, v, to);
+    go(p, v, to);
   };
   const long long da = PA ? g.I * 64 : (AR ? BK : BK * g.lda) * 2, db = PB ? g.J * 64LL : (BR ? BK : BK * g.ldb) * 2;
   // To the next step, in three pieces that fit beside a product each.  (Left alone, the compiler makes all of them at the loop's end, where nothing
@@ -361,58 +378,65 @@ __global__ __launch_bounds__(kThreads, WGS) void gemm_tile_kernel(TileArgs g) {
   };
 
   // ---- fragments from LDS: eight consecutive steps of the reduction of one index per lane, as they lie or by two transpose reads
-  const int lr = lane & 31, lg = lane >> 5;
-  int oa[AR ? NK : TM], ob[BR ? NK : TN];
+  const int lr = lane % FR, lg = lane / FR;
+  int oa[AR ? NK : FM], ob[BR ? NK : FN];
+  auto frag_r = [&](int at, int k, int row_bytes, int swizzle) { return (at + lr) * row_bytes + (((k * (FK / 8) + lg) ^ swizzle) << 4); };
+  const int fr = lg * 8 + ((lane & 15) >> 2), fc = (FR == 32 ? ((lane >> 4) & 1) * 16 : 0) + (lane & 3) * 4;
+  auto frag_t = [&](int at, int row_bytes, int swizzle) { return fr * row_bytes + ((((at + fc) >> 3) ^ swizzle) << 4) + ((at + fc) & 7) * 2; };
   if constexpr (AR) {
 #pragma unroll
-    for (int k = 0; k < NK; ++k) oa[k] = (wm * WTM + lr) * SA::kRow + (((k * 2 + lg) ^ SA::swizzle(lr)) << 4);
+    for (int k = 0; k < NK; ++k) oa[k] = frag_r(wm * WTM, k, SA::kRow, SA::swizzle(lr));
   } else {
-    const int fr = lg * 8 + ((lane & 15) >> 2), fc = ((lane >> 4) & 1) * 16 + (lane & 3) * 4;
 #pragma unroll
-    for (int i = 0; i < TM; ++i) {
-      const int c = wm * WTM + i * 32 + fc;
-      oa[i] = fr * SA::kRow + (((c >> 3) ^ SA::swizzle(fr)) << 4) + (c & 7) * 2;
-    }
+    for (int i = 0; i < FM; ++i) oa[i] = frag_t(wm * WTM + i * FR, SA::kRow, SA::swizzle(fr));
   }
   if constexpr (BR) {
 #pragma unroll
-    for (int k = 0; k < NK; ++k) ob[k] = (wn * WTN + lr) * SB::kRow + (((k * 2 + lg) ^ SB::swizzle(lr)) << 4);
+    for (int k = 0; k < NK; ++k) ob[k] = frag_r(wn * WTN, k, SB::kRow, SB::swizzle(lr));
   } else {
-    const int fr = lg * 8 + ((lane & 15) >> 2), fc = ((lane >> 4) & 1) * 16 + (lane & 3) * 4;
 #pragma unroll
-    for (int j = 0; j < TN; ++j) {
-      const int c = wn * WTN + j * 32 + fc;
-      ob[j] = fr * SB::kRow + (((c >> 3) ^ SB::swizzle(fr)) << 4) + (c & 7) * 2;
-    }
+    for (int j = 0; j < FN; ++j) ob[j] = frag_t(wn * WTN + j * FR, SB::kRow, SB::swizzle(fr));
   }
-  bf16x8 fa[SETS][NP][TM], fb[SETS][NP][TN];
-  constexpr int kFrags = NP * (TM + TN);
-  auto fetch = [&](int n, int set, int stage, int k) {   // fragment n, plane by plane from the smallest part on, of a plane A's first, B's, the rest of A's
-    const int p = NP - 1 - n / (TM + TN), m = n % (TM + TN);
-    const char *A = lds + stage * kStage + p * SA::kBytes, *B = lds + stage * kStage + kA + p * SB::kBytes;
-    if (m == 0 || m > TN) {
-      const int i = m == 0 ? 0 : m - TN;
-      if constexpr (AR) fa[set][p][i] = *reinterpret_cast<const bf16x8 *>(A + oa[k] + i * 32 * SA::kRow);
-      else fa[set][p][i] = lds_read_tr_pair(A + oa[i] + k * 16 * SA::kRow, A + oa[i] + (k * 16 + 4) * SA::kRow);
+  bf16x8 fa[2][NP][FM], fb[2][NP][FN];
+  constexpr int kFrags = NP * (FM + FN);
+  auto fetch_a = [&](int i, int p, int set, int stage, int k) {
+    const char *A = lds + stage * kStage + p * SA::kBytes;
+    if constexpr (AR) fa[set][p][i] = *reinterpret_cast<const bf16x8 *>(A + oa[k] + i * FR * SA::kRow);
+    else fa[set][p][i] = lds_read_tr_pair(A + oa[i] + k * FK * SA::kRow, A + oa[i] + (k * FK + 4) * SA::kRow);
+  };
+  auto fetch_b = [&](int j, int p, int set, int stage, int k) {
+    const char *B = lds + stage * kStage + kA + p * SB::kBytes;
+    if constexpr (BR) fb[set][p][j] = *reinterpret_cast<const bf16x8 *>(B + ob[k] + j * FR * SB::kRow);
+    else fb[set][p][j] = lds_read_tr_pair(B + ob[j] + k * FK * SB::kRow, B + ob[j] + (k * FK + 4) * SB::kRow);
+  };
+  // Fragment n: plane by plane from the smallest part on, of a plane A's first, B's, the rest of A's.  Early, half of A's and of B's in that order, then the
+  // rest of B's, the rest of A's.
+  auto fetch = [&](int n, int set, int stage, int k) {
+    if constexpr (EARLY) {
+      if (n == 0) fetch_a(0, 0, set, stage, k);
+      else if (n <= FN / 2) fetch_b(n - 1, 0, set, stage, k);
+      else if (n < FN / 2 + FM / 2) fetch_a(n - FN / 2, 0, set, stage, k);
+      else if (n < FN + FM / 2) fetch_b(n - FM / 2, 0, set, stage, k);
+      else fetch_a(n - FN, 0, set, stage, k);
     } else {
-      const int j = m - 1;
-      if constexpr (BR) fb[set][p][j] = *reinterpret_cast<const bf16x8 *>(B + ob[k] + j * 32 * SB::kRow);
-      else fb[set][p][j] = lds_read_tr_pair(B + ob[j] + k * 16 * SB::kRow, B + ob[j] + (k * 16 + 4) * SB::kRow);
+      const int p = NP - 1 - n / (FM + FN), m = n % (FM + FN);
+      if (m == 0 || m > FN) fetch_a(m == 0 ? 0 : m - FN, p, set, stage, k);
+      else fetch_b(m - 1, p, set, stage, k);
     }
   };
 
-  f32x16 acc[TM][TN];
+  std::conditional_t<FR == 16, f32x4, f32x16> acc[FM][FN];   // a lane's: 4 or 16 columns, in runs of four, of row lr
 #pragma unroll
-  for (int i = 0; i < TM; ++i)
+  for (int i = 0; i < FM; ++i)
 #pragma unroll
-    for (int j = 0; j < TN; ++j)
+    for (int j = 0; j < FN; ++j)
 #pragma unroll
-      for (int e = 0; e < 16; ++e) acc[i][j][e] = 0.f;
+      for (int e = 0; e < FR * FR / 64; ++e) acc[i][j][e] = 0.f;
 
   // A step of the reduction asks for the tile STAGES steps ahead, whose place in LDS is free once all waves have met: an NK-th of its transfers with
-  // each of NK products of depth 16, from the last of the step before on (early: half with the third and half with the fourth).
+  // each of NK products of depth FK, from the last of the step before on.  Early: all of them in the second of two.
   static_assert((STAGES - 1) * kLoads < 64, "transfers");
-  auto cut = [](int k) constexpr { return (EARLY && 2 * k < NK ? 2 * k : EARLY ? NK : k) * kLoads / NK; };   // a tile's transfers cut(k) .. cut(k + 1) go together
+  auto cut = [](int k) constexpr { return k * kLoads / NK; };   // a tile's transfers cut(k) .. cut(k + 1) go together
 #pragma unroll
   for (int s = 0; s < STAGES - 1; ++s) {
 #pragma unroll
@@ -420,74 +444,99 @@ __global__ __launch_bounds__(kThreads, WGS) void gemm_tile_kernel(TileArgs g) {
 #pragma unroll
     for (int p = 0; p < 3; ++p) advance(p);
   }
-  constexpr int kFirst = cut(EARLY ? 2 : 1);
+  constexpr int kFirst = EARLY ? kLoads : cut(1);
 #pragma unroll
   for (int p = 0; p < kFirst; ++p) request(p, STAGES - 1);
   wait_and_meet<(STAGES - 2) * kLoads + kFirst>();
+  // Early: fragments that a step finds read; the rest go beside its first products (where those are few, there is no time for any)
+  constexpr int kReady = !EARLY || FM * FN < 64 ? kFrags : kFrags / 2;
 #pragma unroll
-  for (int n = 0; n < kFrags; ++n) fetch(n, 0, 0, 0);
+  for (int n = 0; n < kReady; ++n) fetch(n, 0, 0, 0);
   __builtin_amdgcn_sched_barrier(0);
   int stage = 0, refill = STAGES - 1;
-  // sums of a over r (the gradient of a bias): of the steps t with t % tiles_j == tj, the first waves in the even, the second in the odd products
+  // sums of a over r (the gradient of a bias): of the steps t with t % tiles_j == tj, the first waves in the even, the second in the odd products of depth FK
   constexpr bool kSums = !AR && NP == 1;
-  float sums[TM] = {};
+  float sums[FM] = {};
   int sums_at = kSums && g.sums ? tj : 0x7fffffff;
-  auto step = [&](auto kc, int next, bool take) {
-    constexpr int k = decltype(kc)::value, PAIRS = NP == 3 ? 6 : 1, MF = PAIRS * TM * TN, MD = MF > 1 ? MF * 3 / 4 : 1, MH = EARLY || MF == 1 ? MF : MF / 2;
-    constexpr bool last = k + 1 == NK;
-    constexpr int set = EARLY ? k : k & 1;
-    if constexpr (EARLY && k == 2) meet();      // everyone has read this stage
-    if constexpr (last) {
-      if constexpr (!EARLY) {
+  auto sum_up = [&](int set) {
 #pragma unroll
-        for (int p = 0; p < 3; ++p) advance(p);
-      }
-      wait_and_meet<EARLY ? cut(1) : (STAGES - 2) * kLoads>();   // the next stage is there
+    for (int i = 0; i < FM; ++i)
+#pragma unroll
+      for (int e = 0; e < 8; ++e) sums[i] += (float)fa[set][0][i][e];
+  };
+  auto multiply = [](auto &c, const bf16x8 &b, const bf16x8 &a) {
+    if constexpr (sizeof(c) == 16) c = __builtin_amdgcn_mfma_f32_16x16x32_bf16(b, a, c, 0, 0, 0);
+    else c = __builtin_amdgcn_mfma_f32_32x32x16_bf16(b, a, c, 0, 0, 0);
+  };
+  auto step = [&](auto kc, int next, bool take) {
+    constexpr int k = decltype(kc)::value, PAIRS = NP == 3 ? 6 : 1, MF = PAIRS * FM * FN, MD = MF > 1 ? MF * 3 / 4 : 1, MH = MF == 1 ? MF : MF / 2;
+    constexpr bool last = k + 1 == NK;
+    constexpr int set = k & 1, part = (k + 1) % NK, v0 = cut(part), VM = cut(part + 1) - v0, DS = kFrags;
+    if constexpr (last) {
+#pragma unroll
+      for (int p = 0; p < 3; ++p) advance(p);
+      wait_and_meet<(STAGES - 2) * kLoads>();   // the next stage is there
     }
-    // fragments read beside these products: the next one's; early, of the 3 kFrags that are left of this step half with each of its first two
-    // products, and with the last one the next step's first
-    constexpr int d0 = EARLY && k < 2 ? k * 3 * kFrags / 2 : 0, d1 = EARLY ? (k < 2 ? (k + 1) * 3 * kFrags / 2 : last ? kFrags : 0) : kFrags, DS = d1 - d0;
-    constexpr int part = EARLY ? (k + 2) % NK : (k + 1) % NK, v0 = cut(part), VM = cut(part + 1) - v0;
-    int ds = 0, vm = 0;
+    int ds = 0, vm = 0;   // the next product's fragments are read beside this one's
 #pragma unroll
     for (int m = 0; m < MF; ++m) {   // a product, then what goes on beside it, in this order
-      const int pair = m / (TM * TN), i = m / TN % TM, j = m % TN;
+      const int pair = m / (FM * FN), i = m / FN % FM, j = m % FN;
       const int pa_ = NP == 1 ? 0 : pair == 0 ? 2 : pair == 1 ? 0 : pair == 2 ? 1 : pair == 3 ? 1 : 0;   // parts l h', h l', m m', m h', h m', h h'
       const int pb_ = NP == 1 ? 0 : pair == 0 ? 0 : pair == 1 ? 2 : pair == 2 ? 1 : pair == 3 ? 0 : pair == 4 ? 1 : 0;
-      acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fb[set][pb_][j], fa[set][pa_][i], acc[i][j], 0, 0, 0);
+      multiply(acc[i][j], fb[set][pb_][j], fa[set][pa_][i]);
 #pragma unroll
-      for (; ds < (m + 1 < MD ? (m + 1) * DS / MD : DS); ++ds) {
-        if constexpr (EARLY && !last) fetch((d0 + ds) % kFrags, 1 + (d0 + ds) / kFrags, stage, 1 + (d0 + ds) / kFrags);
-        else if constexpr (EARLY) fetch(ds, 0, next, 0);
-        else fetch(ds, (k + 1) & 1, last ? next : stage, last ? 0 : k + 1);
-      }
-      if constexpr (EARLY && k == 1)
-        if (m + 3 >= MF) advance(m + 3 - MF);
+      for (; ds < (m + 1 < MD ? (m + 1) * DS / MD : DS); ++ds) fetch(ds, (k + 1) & 1, last ? next : stage, last ? 0 : k + 1);
 #pragma unroll
-      for (; vm < (m + 1 < MH ? (m + 1) * VM / MH : VM); ++vm) {
-        if constexpr (EARLY) request(v0 + vm, stage);
-        else request(v0 + vm, last ? stage : refill);
-      }
+      for (; vm < (m + 1 < MH ? (m + 1) * VM / MH : VM); ++vm) request(v0 + vm, last ? stage : refill);
       __builtin_amdgcn_sched_barrier(0);
     }
-    if constexpr (kSums) {
-      if (take && (k & 1) == wn) {
-#pragma unroll
-        for (int i = 0; i < TM; ++i)
-#pragma unroll
-          for (int e = 0; e < 8; ++e) sums[i] += (float)fa[set][0][i][e];
-      }
-    }
+    if constexpr (kSums)
+      if (take && (k & 1) == wn) sum_up(set);
+  };
+  // Early: products in four blocks, A's and B's first halves, then B's second, then A's: their fragments may come one after the other.  What goes on
+  // beside a product has 12 clocks, three instructions, so a transfer takes two products' (its address, then itself).
+  auto early_step = [&](auto kc, int next, bool take) {
+    constexpr int k = decltype(kc)::value, P = FM * FN, HM = FM / 2, HN = FN / 2, MD = P * 3 / 4, LATE = kFrags - kReady, VH = kLoads / 2, EACH = EARLY ? P / 2 / VH : 2;
+    static_assert(!EARLY || (EACH >= 2 && NK == 2), "transfers");
+    unsigned v = 0, to = 0;
+    auto due = [](int m) constexpr {   // fragments read before product m
+      if (k == 0) return m < MD ? m * (LATE + kFrags) / MD : LATE + kFrags;
+      return m < P / 2 ? 0 : m < P / 2 + MD / 2 ? (m - P / 2) * kReady / (MD / 2) : kReady;
+    };
+    each(std::make_integer_sequence<int, P>{}, [&](auto mc) {
+      constexpr int m = decltype(mc)::value, b = m / (P / 4), q = m % (P / 4), d0 = due(m), d1 = due(m + 1);
+      constexpr int i = b == 0 ? q / HN : b == 1 ? q % HM : b == 2 ? HM + q / HN : HM + q % HM, j = b == 0 ? q % HN : b == 1 ? HN + q / HM : b == 2 ? HN + q % HN : q / HM;
+      if constexpr (k == 1 && m == 0) meet();                  // everyone has read this stage
+      if constexpr (k == 1 && m == P / 2) wait_and_meet<VH>(); // the next stage is there
+      multiply(acc[i][j], fb[k][0][j], fa[k][0][i]);
+      each(std::make_integer_sequence<int, d1 - d0>{}, [&](auto dc) {
+        constexpr int d = d0 + decltype(dc)::value;
+        if constexpr (k == 1) fetch(d, 0, next, 0);            // the next step's first
+        else if constexpr (d < LATE) fetch(kReady + d, 0, stage, 0);   // what is missing of this product's
+        else fetch(d - LATE, 1, stage, 1);                     // the next one's
+      });
+      if constexpr (k == 0 && m + 3 >= P) advance(m + 3 - P);
+      if constexpr (k == 1 && m % EACH == EACH - 2) aim(m / EACH, stage, v, to);
+      if constexpr (k == 1 && m % EACH == EACH - 1) go(m / EACH, v, to);
+      __builtin_amdgcn_sched_barrier(0);
+    });
+    if constexpr (kSums)
+      if (take && k == wn) sum_up(k);
   };
   for (int t = 0; t < steps; ++t) {
     const int next = stage + 1 == STAGES ? 0 : stage + 1;
     const bool take = kSums && t == sums_at;
     if (take) sums_at += g.tiles_j;
-    step(std::integral_constant<int, 0>{}, next, take);
-    step(std::integral_constant<int, 1>{}, next, take);
-    if constexpr (NK > 2) {
-      step(std::integral_constant<int, 2>{}, next, take);
-      step(std::integral_constant<int, 3>{}, next, take);
+    if constexpr (EARLY) {
+      early_step(std::integral_constant<int, 0>{}, next, take);
+      early_step(std::integral_constant<int, 1>{}, next, take);
+    } else {
+      step(std::integral_constant<int, 0>{}, next, take);
+      step(std::integral_constant<int, 1>{}, next, take);
+      if constexpr (NK > 2) {
+        step(std::integral_constant<int, 2>{}, next, take);
+        step(std::integral_constant<int, 3>{}, next, take);
+      }
     }
     refill = stage;
     stage = next;
@@ -501,9 +550,10 @@ __global__ __launch_bounds__(kThreads, WGS) void gemm_tile_kernel(TileArgs g) {
     if (g.sums) {
       float *to = g.sums + ((size_t)(split * g.tiles_j + tj) * 2 + wn) * g.I;
 #pragma unroll
-      for (int i = 0; i < TM; ++i) {
-        const float s = sums[i] + __shfl_xor(sums[i], 32, 64);
-        const long long at = i0 + wm * WTM + i * 32 + lr;
+      for (int i = 0; i < FM; ++i) {
+        float s = sums[i] + __shfl_xor(sums[i], 32, 64);
+        if (FR == 16) s += __shfl_xor(s, 16, 64);
+        const long long at = i0 + wm * WTM + i * FR + lr;
         if (lg == 0 && at < g.I) to[at] = s;
       }
     }
@@ -511,9 +561,9 @@ __global__ __launch_bounds__(kThreads, WGS) void gemm_tile_kernel(TileArgs g) {
   if constexpr (NP == 3) {
     int bad = 0;
 #pragma unroll
-    for (int i = 0; i < TM; ++i)
+    for (int i = 0; i < FM; ++i)
 #pragma unroll
-      for (int j = 0; j < TN; ++j)
+      for (int j = 0; j < FN; ++j)
 #pragma unroll
         for (int e = 0; e < 16; ++e) bad |= !(fabsf(acc[i][j][e]) <= 3.4028234e38f);
     // the blocks of 64x64 whose values went into this tile
@@ -549,11 +599,14 @@ __global__ __launch_bounds__(kThreads, WGS) void gemm_tile_kernel(TileArgs g) {
   auto put = [&](auto kc) {
     constexpr int k = decltype(kc)::value;
 #pragma unroll
-    for (int n = 0; n < TN; ++n)
+    for (int i = 0; i < 32 / FR; ++i)
 #pragma unroll
-      for (int q = 0; q < 4; ++q)
-        *reinterpret_cast<f32x4 *>(mine + lr * kPitch + (n * 32 + q * 8 + lg * 4) * 4) =
-            f32x4{acc[k][n][q * 4], acc[k][n][q * 4 + 1], acc[k][n][q * 4 + 2], acc[k][n][q * 4 + 3]};
+      for (int n = 0; n < FN; ++n)
+#pragma unroll
+        for (int q = 0; q < FR * FR / 256; ++q) {
+          const auto &c = acc[k * (32 / FR) + i][n];
+          *reinterpret_cast<f32x4 *>(mine + (i * FR + lr) * kPitch + (n * FR + q * 8 + lg * 4) * 4) = f32x4{c[q * 4], c[q * 4 + 1], c[q * 4 + 2], c[q * 4 + 3]};
+        }
     asm volatile("" ::"n"(k));   // left alone, the compiler makes one of the calls, with an index, and keeps the sums in memory for it
   };
   auto meet_lanes = [&]() {   // LDS takes a wave's accesses in order: it is the compiler that has to
