@@ -1015,17 +1015,17 @@ FewPlan plan_few(int dt, int op, long long M, int J, int R) {
 
 // Which tiles, and how many ranges of the reduction (`splits`): the least time by a model of the kernels, us, with what was measured alone on the chip:
 // a launch, then rounds of as many workgroups as fit (one or two a CU), each its start and epilogue and `step` per 64 of the reduction
-// (`low` with a quarter of that many, `full` with all: the clock gives way under the products); a split reduction writes
-// its parts and reads them back in a launch of its own.  Either side of the choice, us measured, bf16 forward unless said
+// (`low` with a quarter of that many, `half`, `full` with all: the clock gives way under the products, and two share a CU); a split reduction writes
+// its parts and reads them back, from a cache, in a launch of its own.  Either side of the choice, us measured, bf16 forward unless said
 // (M x K x N: 256x256 | 128x128 | 64x64):
 //   8192x8192x2048  202 | 246 | 427     4096x2048x2048  47 | 37 | 60     512x4096x4096  77 | 43 | 31      64x512x512  16 | 8.1 | 6.1
 //   128x4096x512, 64x64: 1 split 22.2, 2 15.4, 4 11.8, 8 11.3            128x512x4096, 64x64: 1 split 6.4, 2 9.9, 4 12.0
 //   fp32 (256x128 | 128x128 | 64x64)  8192x2048x2048  324 | 335 | 383     2048x1024x4096  92 | 97 | 106     2000x1024x1024  63 | 45 (2 splits 40) | 36
-struct TileCost { int bm, bn, fit; double start, low, full; };
+struct TileCost { int bm, bn, fit; double start, low, half, full; };
 constexpr int kSizes = 3;
-constexpr TileCost kTiles[2][kSizes] = {{{256, 256, 256, 7.0, 1.15, 1.58}, {128, 128, 512, 2.6, 0.58, 1.03}, {64, 64, 512, 1.4, 0.28, 0.42}},
-                                   {{256, 128, 256, 5.0, 2.9, 4.6}, {128, 128, 256, 3.0, 1.6, 2.4}, {64, 64, 512, 1.5, 0.65, 1.55}}};
-constexpr double kLaunch = 2.0, kJoin = 3.0, kBytesPerUs = 3.5e6;
+constexpr TileCost kTiles[2][kSizes] = {{{256, 256, 256, 10.0, 1.1, 1.25, 1.41}, {128, 128, 512, 4.0, 0.5, 0.53, 0.91}, {64, 64, 512, 1.4, 0.26, 0.27, 0.41}},
+                                   {{256, 128, 256, 5.0, 2.9, 3.75, 4.6}, {128, 128, 256, 3.0, 1.6, 2.0, 2.4}, {64, 64, 512, 1.5, 0.65, 0.9, 1.55}}};
+constexpr double kLaunch = 2.0, kJoin = 3.0, kBytesPerUs = 8e6;
 struct Plan {
   int size;                  // of the tiles: an index into kTiles
   int bm, bn, splits;
@@ -1043,7 +1043,7 @@ Plan plan_tiles(int np, long long I, long long J, long long R) {
       const long long per = (steps + want - 1) / want, splits = (steps + per - 1) / per, wgs = tiles * splits;
       const long long rounds = wgs / c.fit, rest = wgs - rounds * c.fit;
       double t = kLaunch + rounds * (c.start + per * c.full);
-      if (rest > 0) t += c.start + per * (rest * 4 <= c.fit ? c.low : rest * 2 <= c.fit ? 0.5 * (c.low + c.full) : c.full);
+      if (rest > 0) t += c.start + per * (rest * 4 <= c.fit ? c.low : rest * 2 <= c.fit ? c.half : c.full);
       if (splits > 1) t += kJoin + 8. * splits * I * J / kBytesPerUs;
       if (best.splits == 0 || t < least) {
         least = t;
