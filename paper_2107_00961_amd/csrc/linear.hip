@@ -761,11 +761,14 @@ __global__ __launch_bounds__(kThreads) void gemm_join_kernel(JoinArgs a) {
   if (side) raw_load(side + row * ld + j, left, now[0]);
   float v[1][8];
   row_load(a.part + row * a.J + j, left, v[0]);
-  for (int s = 1; s < a.splits; ++s) {
-    float w[8];
-    row_load(a.part + ((long long)s * a.I + row) * a.J + j, left, w);
+  for (int s = 1; s < a.splits; s += 3) {   // three on their way at once (past the last one that again)
+    float w[3][8];
 #pragma unroll
-    for (int k = 0; k < 8; ++k) v[0][k] += w[k];
+    for (int u = 0; u < 3; ++u) row_load(a.part + ((long long)min(s + u, a.splits - 1) * a.I + row) * a.J + j, left, w[u]);
+#pragma unroll
+    for (int u = 0; u < 3; ++u)
+#pragma unroll
+      for (int k = 0; k < 8; ++k) v[0][k] += s + u < a.splits ? w[u][k] : 0.f;
   }
   O *const out[1] = {static_cast<O *>(a.e.out) + row * a.e.ldo + j}, *const z_out[1] = {static_cast<O *>(a.e.z_out) + row * a.e.ldz + j};
   const u64 word[1] = {a.e.d.rng ? dropout_base(a.e.d.rng) + ((u64)row * (unsigned)a.e.words + (unsigned)(j >> 1)) * kGolden : 0};
@@ -991,9 +994,9 @@ __global__ __launch_bounds__(kThreads) void few_rows_wgrad_kernel(const T *dz, l
 
 // ---- plans ----------------------------------------------------------------------------------------------------------
 // Up to this many rows go without tiles.  us, 4096 -> 4096, tiles (with what they lay out and join) -> few rows:
-//   fp32 1 row: forward 50 -> 15, data gradient 54 -> 16, weight gradient 34 -> 13      17 rows: 50 -> 20, 55 -> 19, 34 (tiles)
-//   fp32 64 rows: 51 -> 39, 55 -> 40     bf16 1 row: forward 11.4 -> 7.4 (4.5 TB/s), data gradient 11.5 (tiles; 40 with 64 columns to a workgroup), weight gradient 27 -> 13.5 (5 TB/s)
-//   bf16 16 rows: forward 12.7 -> 10.1, weight gradient 27 -> 16     32 rows: forward 13.3 -> 14.1, at 512 -> 512 6.0 -> 4.5
+//   fp32 1 row: forward 50 -> 15, data gradient 53 -> 16, weight gradient 33 -> 13      17 rows: 50 -> 20, 55 -> 20, 34 (tiles)
+//   fp32 64 rows: 51 -> 39, 55 -> 41     bf16 1 row: forward 11.6 -> 7.4 (4.5 TB/s), data gradient 11 (tiles; 40 with 64 columns to a workgroup), weight gradient 23 -> 13.4 (5 TB/s)
+//   bf16 16 rows: forward 12.5 -> 10.1, weight gradient 24 -> 16.5     32 rows: forward 13.2 -> 14.1, at 512 -> 512 5.4 -> 4.5
 int few(int dt, int op) {
   if (op == 2) return 16;
   return dt == DT_F32 ? 64 : op == 0 ? 32 : 0;
@@ -1018,14 +1021,14 @@ FewPlan plan_few(int dt, int op, long long M, int J, int R) {
 // (`low` with a quarter of that many, `half`, `full` with all: the clock gives way under the products, and two share a CU); a split reduction writes
 // its parts and reads them back, from a cache, in a launch of its own.  Either side of the choice, us measured, bf16 forward unless said
 // (M x K x N: 256x256 | 128x128 | 64x64):
-//   8192x8192x2048  202 | 246 | 427     4096x2048x2048  47 | 37 | 60     512x4096x4096  77 | 43 | 31      64x512x512  16 | 8.1 | 6.1
-//   128x4096x512, 64x64: 1 split 22.2, 2 15.4, 4 11.8, 8 11.3            128x512x4096, 64x64: 1 split 6.4, 2 9.9, 4 12.0
-//   fp32 (256x128 | 128x128 | 64x64)  8192x2048x2048  324 | 335 | 383     2048x1024x4096  92 | 97 | 106     2000x1024x1024  63 | 45 (2 splits 40) | 36
+//   8192x8192x2048  190 | 230 | 389     4096x2048x2048  46 | 35 | 55     512x4096x4096  76 | 35 | 28      64x512x512  16 | 7.9 | 5.4
+//   128x4096x512, 64x64: 1 split 17.7, 2 13.4, 4 10.1, 8 10.0, 16 11.5   128x512x4096, 64x64: 1 split 5.7, 2 9.5, 4 11.7
+//   fp32 (256x128 | 128x128 | 64x64)  8192x2048x2048  329 | 345 | 397     2048x1024x4096  94 | 99 | 109     2000x1024x1024  62 | 46 (2 splits 40) | 36
 struct TileCost { int bm, bn, fit; double start, low, half, full; };
 constexpr int kSizes = 3;
 constexpr TileCost kTiles[2][kSizes] = {{{256, 256, 256, 10.0, 1.1, 1.25, 1.41}, {128, 128, 512, 4.0, 0.5, 0.53, 0.91}, {64, 64, 512, 1.4, 0.26, 0.27, 0.41}},
-                                   {{256, 128, 256, 5.0, 2.9, 3.75, 4.6}, {128, 128, 256, 3.0, 1.6, 2.0, 2.4}, {64, 64, 512, 1.5, 0.65, 0.9, 1.55}}};
-constexpr double kLaunch = 2.0, kJoin = 3.0, kBytesPerUs = 8e6;
+                                   {{256, 128, 256, 5.0, 2.9, 3.75, 4.6}, {128, 128, 256, 9.0, 1.5, 1.6, 2.15}, {64, 64, 512, 1.5, 0.65, 0.9, 1.55}}};
+constexpr double kLaunch = 2.0, kJoin = 2.5, kJoinPart = 0.4, kBytesPerUs = 8e6;
 struct Plan {
   int size;                  // of the tiles: an index into kTiles
   int bm, bn, splits;
@@ -1044,7 +1047,7 @@ Plan plan_tiles(int np, long long I, long long J, long long R) {
       const long long rounds = wgs / c.fit, rest = wgs - rounds * c.fit;
       double t = kLaunch + rounds * (c.start + per * c.full);
       if (rest > 0) t += c.start + per * (rest * 4 <= c.fit ? c.low : rest * 2 <= c.fit ? c.half : c.full);
-      if (splits > 1) t += kJoin + 8. * splits * I * J / kBytesPerUs;
+      if (splits > 1) t += kJoin + kJoinPart * splits + 8. * splits * I * J / kBytesPerUs;
       if (best.splits == 0 || t < least) {
         least = t;
         best = Plan{size, c.bm, c.bn, (int)splits, per * 64};
