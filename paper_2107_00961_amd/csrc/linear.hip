@@ -129,9 +129,9 @@ __global__ __launch_bounds__(kThreads) void lay_out_kernel(LayOutArgs a) {
 // Operand tiles go from memory straight into LDS (16 bytes a lane, 1 KB a wave and instruction, in lane order), STAGES deep, and from there
 // in fragments to the matrix cores.  Four waves, a quarter of the BM x BN tile each: the larger a wave's share, the fewer times a
 // staged element is read from LDS (256x256: 1024 clocks of reading and 512 of arriving for 2048 of products).  Bound by the matrix cores and what
-// the chip's power leaves of its clock: 8192 x 8192 -> 2048 in bf16 201 ... 210 us (1.35 PFLOP/s, the cores at work in 74 % of 357 thousand clocks at 1.7 GHz),
-// 2000 x 1024 -> 1024 in fp32 30 us beside 8 of laying out.  The epilogue's arithmetic is not hidden, one workgroup having a compute unit to itself: through GELU and
-// dropout 8192 x 2048 -> 8192 takes 300 us for 227, and making the mask between the products, though it fits, 297.
+// the chip's power leaves of its clock: 8192 x 8192 -> 2048 in bf16 192 us (1.43 PFLOP/s, the cores at work in 72 % of 362 thousand clocks at 1.86 GHz),
+// 2000 x 1024 -> 1024 in fp32 30 us beside 8 of laying out.  The epilogue's arithmetic is not hidden, one workgroup having a compute unit to itself: with GELU,
+// dropout and z 8192 x 2048 -> 8192 takes 282 ... 294 us for 213 ... 240 (making the mask between the products, though it fits, saved 1 %).
 // Layout in LDS.  Lane order leaves no room for padding, so what keeps rows off each other's banks is which 16-byte piece a lane asks for:
 //   reduction contiguous (R): a row is an index i, BK values of r: piece c of row i lies at c ^ f(i), f = (i >> 1) & 7 (BK 64, two rows to 256
 //     bytes), (i >> 2) & 3 (BK 32, four rows): sixteen consecutive rows' pieces c fill the 256 bytes of the 64 banks;
