@@ -170,33 +170,17 @@ __device__ inline float upper_tail_over(float x, float &e) {
   e = exp2_f(x * x * (-0.5f * kLog2e));
   return p * t;
 }
-// Phi(z) to 3e-5 of itself for |z| < 3, and z Phi(z) to 1e-6 beyond: the logistic of an odd polynomial of degree 9 (fitted to log Phi(z)/Phi(-z)
-// with that allowance), for results that are rounded to bf16 (2^-9 of themselves).  Half the instructions of upper_tail_over.
-__device__ inline float phi_coarse(float z) {
-  const float q = z * z;
-  float p = 2.0995009433e-06f;
-  p = __builtin_fmaf(p, q, -5.7487801011e-05f);
-  p = __builtin_fmaf(p, q, -2.7864286929e-04f);
-  p = __builtin_fmaf(p, q, 7.3012652228e-02f);
-  p = __builtin_fmaf(p, q, 1.5956096079f);
-  return sigmoid_f(z * p);
-}
-// COARSE: the results are rounded to bf16
-template <bool COARSE, int V> __device__ inline void activate(float (&v)[V], int act) {
+template <int V> __device__ inline void activate(float (&v)[V], int act) {
   if (act == RESIST_ACT_RELU) {
 #pragma unroll
     for (int k = 0; k < V; ++k) v[k] = v[k] > 0.f ? v[k] : 0.f;
   } else if (act == RESIST_ACT_GELU) {   // z - z Q(z), or z Q(-z)
 #pragma unroll
     for (int k = 0; k < V; ++k) {
-      if constexpr (COARSE) {
-        v[k] *= phi_coarse(v[k]);
-      } else {
-        const float z = v[k], x = fabsf(z) > 20.f ? 20.f : fabsf(z);
-        float e;
-        const float q = upper_tail_over(x, e);
-        v[k] = (z > 0.f ? z : 0.f) - x * q * e;
-      }
+      const float z = v[k], x = fabsf(z) > 20.f ? 20.f : fabsf(z);
+      float e;
+      const float q = upper_tail_over(x, e);
+      v[k] = (z > 0.f ? z : 0.f) - x * q * e;
     }
   } else if (act == RESIST_ACT_GELU_TANH) {
 #pragma unroll

@@ -36,7 +36,7 @@ __device__ inline void finish(const Epilogue &e, long long i, int j, float v, u6
   float t[1] = {v};
   if (e.bias) t[0] += e.bias[j];
   if (e.z_out) static_cast<T *>(e.z_out)[i * e.ldz + j] = (T)t[0];
-  if (!e.z_in) activate<sizeof(T) == 2>(t, e.act);
+  if (!e.z_in) activate(t, e.act);
   if (e.d.rng) {
     const u64 w = splitmix(base + ((u64)i * (unsigned)e.words + (unsigned)(j >> 1)) * kGolden);
     t[0] = (unsigned)(j & 1 ? w >> 32 : w) < e.d.thr ? 0.f : t[0] * e.d.scale;
@@ -131,7 +131,7 @@ __global__ __launch_bounds__(kThreads) void lay_out_kernel(LayOutArgs a) {
 // staged element is read from LDS (256x256: 1024 clocks of reading and 512 of arriving for 2048 of products).  Bound by the matrix cores and what
 // the chip's power leaves of its clock: 8192 x 8192 -> 2048 in bf16 192 us (1.43 PFLOP/s, the cores at work in 72 % of 362 thousand clocks at 1.86 GHz),
 // 2000 x 1024 -> 1024 in fp32 30 us beside 8 of laying out.  The epilogue's arithmetic is not hidden, one workgroup having a compute unit to itself: with GELU,
-// dropout and z 8192 x 2048 -> 8192 takes 282 ... 294 us for 213 ... 240 (making the mask between the products, though it fits, saved 1 %).
+// dropout and z 8192 x 2048 -> 8192 takes 290 ... 305 us for 213 ... 240 (making the mask between the products, though it fits, saved 1 %).
 // Layout in LDS.  Lane order leaves no room for padding, so what keeps rows off each other's banks is which 16-byte piece a lane asks for:
 //   reduction contiguous (R): a row is an index i, BK values of r: piece c of row i lies at c ^ f(i), f = (i >> 1) & 7 (BK 64, two rows to 256
 //     bytes), (i >> 2) & 3 (BK 32, four rows): sixteen consecutive rows' pieces c fill the 256 bytes of the 64 banks;
@@ -195,7 +195,7 @@ __device__ inline void finish_rows(const Epilogue &e, O *const (&out)[H], O *con
   };
   float(&all)[H * 8] = reinterpret_cast<float(&)[H * 8]>(v);
   if (e.z_out) store(z_out);
-  if (!e.z_in) activate<sizeof(O) == 2>(all, e.act);
+  if (!e.z_in) activate(all, e.act);
   if (e.d.rng) {
 #pragma unroll
     for (int h = 0; h < H; ++h) dropout8(word[h], e.d.thr, e.d.scale, v[h]);

@@ -1,0 +1,56 @@
+"""GPU: the dense operators where their arguments go to an end: activations far out and where z is not finite, more rows than one launch takes, rows
+very far apart, layer norm in place in rows of every kind, a block's gradients from the activations it kept.
+
+U = 2^-24 is half a step of fp32, 2^-8 of bf16; a bound that counts roundings says which."""
+import ctypes as C
+
+import numpy as np
+import pytest
+import torch
+
+import paper_2107_00961_amd as R
+from oracle import dense as D
+
+pytestmark = pytest.mark.gpu
+
+U = 2.0 ** -24
+DT = {"f32": torch.float32, "bf16": torch.bfloat16}
+HALF = {"f32": U, "bf16": 2.0 ** -8}
+
+
+def host(t):
+    return t.detach().double().cpu().numpy()
+
+
+def near(got, want, tol, what):
+    got = host(got)
+    assert got.shape == want.shape and np.isfinite(got).all(), what
+    over = np.abs(got - want) / np.broadcast_to(tol, want.shape)
+    if (over > 1).any():
+        i = np.unravel_index(np.argmax(over), over.shape)
+        raise AssertionError(f"{what}: {(over > 1).sum()} of {over.size} off; worst at {i}: {got[i]:.9g} for {want[i]:.9g}, {over[i]:.3g} times the tolerance")
+
+
+def function_roundings(z, act):
+    """Roundings U of act(z), relative to it, before it is stored.
+    GELU from Q(x)/e = t p(t), t = 1/(1 + c x), e = exp(-x^2/2): t 4 (c, the sum, a reciprocal within 2), which count 2.7 times in t p(t); p 3.1 for its
+    steps and 1.8 for its coefficients, each as given; the fit 1.7; e 2 and, of an argument with three roundings, 3 x^2/2; products 3.
+    SiLU and the tanh form from 1/(1 + exp(-a)): of a 2 roundings for a = z and 9 for a = 2u (and one each of exp's argument), exp and
+    reciprocal 2 each, sum and product 1 each."""
+    z = np.abs(z)
+    if act == "gelu":
+        return 24 + 1.5 * z * z
+    return 6 + 2 * z if act == "silu" else 7 + 9 * 2 * np.sqrt(2 / np.pi) * z * (1 + 0.044715 * z * z)
+
+
+@pytest.mark.parametrize("dt", ["f32", "bf16"])
+@pytest.mark.parametrize("act", ["gelu", "gelu_tanh", "silu"])
+def test_activations_are_right_relative_to_themselves(act, dt):
+    """Out to where they are no longer normal numbers; as one column (tiles) and as one row (few rows).  The product is z itself."""
+    z = torch.from_numpy(np.concatenate([np.linspace(-13, -0.001, 4097), np.linspace(0.001, 13, 999)]).astype(np.float32)).cuda().to(DT[dt])
+    one = torch.ones(1, 1, device="cuda", dtype=DT[dt])
+    z64 = host(z)
+    want = D.act(z64, act)
+    tol = (HALF[dt] + U * function_roundings(z64, act)) * np.abs(want) + np.abs(z64) * 2.0 ** -125
+    near(R.linear_forward(z[:, None], one, act=act)[:, 0], want, tol, "a column")
+    near(R.linear_forward(one, z[:, None], act=act)[0], want, tol, "a row")
