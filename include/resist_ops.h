@@ -97,6 +97,8 @@ int resist_conv2d_wgrad_static_limit(int64_t *bytes);
  *   RESIST_ACT_GELU       z Phi(z), Phi the normal distribution function
  *   RESIST_ACT_GELU_TANH  z/2 (1 + tanh(sqrt(2/pi) (z + 0.044715 z^3)))
  *   RESIST_ACT_SILU       z / (1 + exp(-z))
+ * Of infinite z all of them and their derivatives are the limits (a(-inf) = 0 but for NONE); a NaN stays one, but for RELU, which
+ * takes what is not above 0 as 0, as in resist.h's layers.
  *
  * Dropout with probability 0 <= p < 1: an element is dropped (0, whatever it was) or kept and multiplied by 1/(1-p).  The mask is never
  * stored: it is a function of rng, device {seed, offset}, read when the kernel runs (a captured call draws a new mask with

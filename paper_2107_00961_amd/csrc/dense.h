@@ -151,7 +151,7 @@ constexpr float kGeluC = 0.7978845608028654f, kGeluK = 0.044715f, kInvSqrt2Pi = 
 __device__ inline float exp2_f(float x) { return __builtin_amdgcn_exp2f(x); }   // one instruction each, within a step
 __device__ inline float rcp_f(float x) { return __builtin_amdgcn_rcpf(x); }
 __device__ inline float sigmoid_f(float x) { return rcp_f(1.f + exp2_f(-kLog2e * x)); }
-// Far out, where Phi and the derivatives are 0 or 1 to the last bit, what grows is held back: it would meet that zero as infinity.  (One
+// Far out, where Phi, the logistic and the derivatives are 0 or 1 to the last bit, what grows is held back: it would meet that zero as infinity.  (One
 // instruction; of a NaN it makes a number, but the other factor is one as well then.)
 __device__ inline float held(float z, float most) { return __builtin_amdgcn_fmed3f(z, -most, most); }
 // Q(x) = 1 - Phi(x) for 0 <= x <= 20, and e = exp(-x^2/2), which is phi(x) sqrt(2 pi).  Q(x)/e, Mills' ratio over sqrt(2 pi), is nearly a
@@ -184,10 +184,10 @@ template <int V> __device__ inline void activate(float (&v)[V], int act) {
     }
   } else if (act == RESIST_ACT_GELU_TANH) {
 #pragma unroll
-    for (int k = 0; k < V; ++k) v[k] = v[k] * sigmoid_f(2.f * kGeluC * (v[k] + kGeluK * v[k] * v[k] * v[k]));
+    for (int k = 0; k < V; ++k) v[k] = fmaxf(v[k], -20.f) * sigmoid_f(2.f * kGeluC * (v[k] + kGeluK * v[k] * v[k] * v[k]));
   } else if (act == RESIST_ACT_SILU) {
 #pragma unroll
-    for (int k = 0; k < V; ++k) v[k] = v[k] * sigmoid_f(v[k]);
+    for (int k = 0; k < V; ++k) v[k] = fmaxf(v[k], -200.f) * sigmoid_f(v[k]);
   }
 }
 // v[k] *= a'(z[k])

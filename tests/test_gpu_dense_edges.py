@@ -54,3 +54,15 @@ def test_activations_are_right_relative_to_themselves(act, dt):
     tol = (HALF[dt] + U * function_roundings(z64, act)) * np.abs(want) + np.abs(z64) * 2.0 ** -125
     near(R.linear_forward(z[:, None], one, act=act)[:, 0], want, tol, "a column")
     near(R.linear_forward(one, z[:, None], act=act)[0], want, tol, "a row")
+
+
+@pytest.mark.parametrize("dt", ["f32", "bf16"])
+@pytest.mark.parametrize("act,want", [("relu", [np.inf, 0.0, 0.0]), ("gelu", [np.inf, 0.0, np.nan]), ("gelu_tanh", [np.inf, 0.0, np.nan]),
+                                      ("silu", [np.inf, 0.0, np.nan])])
+def test_activations_where_z_is_not_finite(act, want, dt):
+    """The limits at both ends; a NaN stays one, but for ReLU, which passes on what is above 0 and nothing else."""
+    z = torch.tensor([np.inf, -np.inf, np.nan] * 40, device="cuda").to(DT[dt])
+    one = torch.ones(1, 1, device="cuda", dtype=DT[dt])
+    want = torch.tensor(want * 40, device="cuda").to(DT[dt])
+    for got in (R.linear_forward(z[:, None], one, act=act)[:, 0], R.linear_forward(one, z[:, None], act=act)[0]):
+        assert torch.equal(got.isnan(), want.isnan()) and torch.equal(got.nan_to_num(7.0), want.nan_to_num(7.0)), got[:3]
