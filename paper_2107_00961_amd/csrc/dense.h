@@ -8,6 +8,8 @@
 
 namespace resist {
 
+constexpr unsigned kMaxThreads = 0xffffffffu;   // of a launch, along an axis
+
 // Rows of a matrix whose stride or width is no multiple of 16 bytes start anywhere an element can: 16-byte accesses that promise no more
 // than the element's own alignment (one instruction each all the same: global memory takes any address).
 typedef f32x4 f32x4_any __attribute__((aligned(4)));

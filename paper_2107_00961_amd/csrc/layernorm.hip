@@ -428,20 +428,43 @@ int bwd_parts(int64_t M, int N) {
     else call((kernel<T, 512, 2>), 512);                                          \
   } while (0)
 
-template <typename T> int fwd(const LnArgs &a, hipStream_t st) {
-  if (a.N > kHeldCols) {
-    ln_fwd_long_kernel<T><<<dim3((unsigned)a.M), kThreads, 0, st>>>(a);
-  } else {
-#define FWD(k, tpr) k<<<(unsigned)((a.M + threads_of(tpr) / tpr - 1) / (threads_of(tpr) / tpr)), threads_of(tpr), 0, st>>>(a)
-    LN_HELD(ln_fwd_kernel, T, a.N, FWD);
+// Rows that one launch takes where a workgroup of `threads` takes `rows`: with 2^32 threads or more it would count them modulo 2^32, and
+// leave rows out without an error.
+long long rows_a_launch(int threads, int rows) { return (long long)(kMaxThreads / threads) * rows; }
+
+template <typename T> int fwd(const LnArgs &all, hipStream_t st) {
+  const int tpr = all.N > kHeldCols ? kThreads : held_shape(all.N).tpr, rpw = threads_of(tpr) / tpr;
+  const long long most = rows_a_launch(threads_of(tpr), rpw);
+  for (long long at = 0; at < all.M; at += most) {
+    LnArgs a = all;
+    a.M = std::min(most, all.M - at);
+    a.x = static_cast<const T *>(all.x) + at * all.ldx;
+    a.out = static_cast<T *>(all.out) + at * all.ldo;
+    if (all.mean) a.mean = all.mean + at;
+    if (all.rstd) a.rstd = all.rstd + at;
+    const unsigned wgs = (unsigned)((a.M + rpw - 1) / rpw);
+    if (a.N > kHeldCols) {
+      ln_fwd_long_kernel<T><<<wgs, kThreads, 0, st>>>(a);
+    } else {
+#define FWD(k, tpr) k<<<wgs, threads_of(tpr), 0, st>>>(a)
+      LN_HELD(ln_fwd_kernel, T, a.N, FWD);
 #undef FWD
+    }
+    RESIST_CHECK_LAUNCH("layernorm_fwd");
   }
-  RESIST_CHECK_LAUNCH("layernorm_fwd");
   return RESIST_OK;
 }
 template <typename T> int bwd(const LnArgs &a, int parts, float *sums, hipStream_t st) {
   if (a.N > kHeldCols) {
-    ln_bwd_rows_kernel<T><<<dim3((unsigned)a.M), kThreads, 0, st>>>(a, sums);
+    const long long most = rows_a_launch(kThreads, 1);
+    for (long long at = 0; at < a.M; at += most) {
+      LnArgs b = a;
+      b.x = static_cast<const T *>(a.x) + at * a.ldx;
+      b.dy = static_cast<const T *>(a.dy) + at * a.lddy;
+      b.mean = a.mean + at;
+      b.rstd = a.rstd + at;
+      ln_bwd_rows_kernel<T><<<(unsigned)std::min(most, a.M - at), kThreads, 0, st>>>(b, sums + 2 * at);
+    }
     ln_bwd_cols_kernel<T><<<dim3(parts, (a.N + kThreads * 8 - 1) / (kThreads * 8)), kThreads, 0, st>>>(a, sums);
   } else {
 #define BWD(k, tpr) k<<<parts, threads_of(tpr), 0, st>>>(a)

@@ -66,3 +66,41 @@ def test_activations_where_z_is_not_finite(act, want, dt):
     want = torch.tensor(want * 40, device="cuda").to(DT[dt])
     for got in (R.linear_forward(z[:, None], one, act=act)[:, 0], R.linear_forward(one, z[:, None], act=act)[0]):
         assert torch.equal(got.isnan(), want.isnan()) and torch.equal(got.nan_to_num(7.0), want.nan_to_num(7.0)), got[:3]
+
+
+# ---- more rows than one launch takes: 2^32 threads -------------------------------------------------------------------------
+def random(m, n, dt, seed):
+    g = torch.Generator(device="cuda").manual_seed(seed)
+    torch.cuda.empty_cache()
+    return torch.empty(m, n, device="cuda", dtype=DT[dt]).normal_(generator=g)
+
+
+def rows_of(m):
+    """The first and the last, and those on either side of multiples of 2^24 - 1 and 2^24 workgroups of 1 to 64 rows."""
+    at = {0, 1, m - 2, m - 1}
+    for shift in range(7):
+        for e in (((1 << 24) - 1) << shift, 1 << 24 + shift, 1 << 23 + shift, ((1 << 23) - 1) << shift):
+            at |= {r for r in (e - 1, e, e + 1) if r < m}
+    return sorted(at)
+
+
+@pytest.mark.parametrize("m,n", [((1 << 28) + 5, 8), ((1 << 26) + 3, 260), ((1 << 23) + 3, 4100)])
+def test_layernorm_of_many_rows(m, n):
+    """16, 64 and 512 threads a row.  Of a row: sums in a tree of 48 steps, the stored value's half step (as in test_gpu_dense.py)."""
+    x = random(m, n, "bf16", 1)
+    y, mean, rstd = R.layernorm_forward(x)
+    at = rows_of(m)
+    x64 = host(x[at])
+    want, mu, r = D.layernorm(x64)
+    e_mean = 48 * U * np.abs(x64).mean(1)
+    rel = 56 * U + e_mean ** 2 * r ** 2
+    near(mean[at], mu, e_mean + U * np.abs(mu), "mean")
+    near(rstd[at], r, rel * r, "rstd")
+    xhat = np.abs(x64 - mu[:, None]) * r[:, None]
+    near(y[at], want, e_mean[:, None] * r[:, None] * (1 + rel[:, None]) + xhat * (rel[:, None] + 6 * U) + (4 * U + HALF["bf16"] * 1.01) * np.abs(want) + 1e-38, "y")
+    # every row's mean, and y's: that of 0 but for y's own roundings, 2^-8 of at most sqrt(n) each
+    step = (1 << 30) // n
+    for i in range(0, m, step):
+        part = x[i:i + step].float()
+        assert ((mean[i:i + step] - part.mean(1)).abs() <= 100 * U * part.abs().mean(1)).all(), i
+        assert (y[i:i + step].float().mean(1).abs() <= 2.0 ** -8).all(), i
