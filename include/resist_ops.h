@@ -141,7 +141,8 @@ int resist_dropout_backward(int64_t M, int32_t N, int32_t dtype, const void *dy,
                             const void *z, int64_t ldz, void *dx, int64_t lddx, void *hip_stream);
 
 /*
- * Dense layer, x [M][K], w [N][K], y [M][N] (1 <= K, N <= 2^20, row strides up to 2^20, M < 2^31):
+ * Dense layer, x [M][K], w [N][K], y [M][N] (1 <= K, N <= 2^20, row strides up to 2^20, M < 2^31; of 2^38 outputs or more, beyond any
+ * card's memory, a call may be refused with RESIST_ESHAPE):
  *   forward          z = x w' + bias,  y = [residual +] drop(act(z))      [y in place of residual]
  *   data gradient    dx = a'(z) drop(dz w): z, act and drop are of the layer that produced x, the gradient leaves taken
  *                    through them                                         [dx in place of z]

@@ -119,8 +119,13 @@ int to_linear(const resist_linear_shape *s, LinearShape *o) {
   RESIST_TRY(check_ld(&o->ldx, s->K, "x", kMaxLinear));
   return check_ld(&o->ldy, s->N, "y", kMaxLinear);
 }
+int work_of(const LinearShape &s, int dt, int op, int64_t *need) {
+  *need = linear_workspace(s, dt, op);
+  return *need < 0 ? set_error(RESIST_ESHAPE, "dense layer of %lld rows, %d inputs and %d outputs", (long long)s.M, s.K, s.N) : RESIST_OK;
+}
 int check_work(const LinearShape &s, int dt, int op, const void *workspace, int64_t bytes) {
-  const int64_t need = linear_workspace(s, dt, op);
+  int64_t need;
+  RESIST_TRY(work_of(s, dt, op, &need));
   if (need == 0) return RESIST_OK;
   RESIST_TRY(check_ptr(workspace, "workspace"));
   return bytes < need ? set_error(RESIST_EWORKSPACE, "workspace of %lld bytes where %lld are needed", (long long)bytes, (long long)need) : RESIST_OK;
@@ -132,8 +137,7 @@ extern "C" int resist_linear_workspace_bytes(const resist_linear_shape *s, int32
   RESIST_TRY(to_linear(s, &l));
   if (op < 0 || op > 2) return set_error(RESIST_EINVAL, "op %d", op);
   if (!bytes) return set_error(RESIST_EINVAL, "bytes is NULL");
-  *bytes = linear_workspace(l, s->dtype, op);
-  return RESIST_OK;
+  return work_of(l, s->dtype, op, bytes);
 }
 
 extern "C" int resist_linear_forward(const resist_linear_shape *s, const void *x, const void *w, const resist_linear_epilogue *epilogue, void *y,

@@ -265,7 +265,7 @@ int dropout(int dt, int64_t M, int N, const void *x, int64_t ldx, const void *re
 struct LinearShape { int64_t M; int K, N; int64_t ldx, ldy; };
 struct LinearEpilogue { const float *bias; int act; DropSpec drop; const void *residual; int64_t ldr; void *z; int64_t ldz; };
 struct LinearThrough { int act; const void *z; int64_t ldz; DropSpec drop; };
-int64_t linear_workspace(const LinearShape &s, int dt, int op);   // bytes; op 0 forward, 1 data gradient, 2 weight gradient
+int64_t linear_workspace(const LinearShape &s, int dt, int op);   // bytes, or -1: too large a call; op 0 forward, 1 data gradient, 2 weight gradient
 int linear_fwd(const LinearShape &s, int dt, const void *x, const void *w, const LinearEpilogue &e, void *y, void *work, hipStream_t st);
 int linear_dgrad(const LinearShape &s, int dt, const void *dz, const void *w, const LinearThrough &t, void *dx, void *work, hipStream_t st);
 int linear_wgrad(const LinearShape &s, int dt, const void *dz, const void *x, float *dw, float *db, void *work, hipStream_t st);

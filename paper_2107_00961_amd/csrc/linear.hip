@@ -17,6 +17,7 @@ namespace resist {
 namespace {
 
 constexpr int kThreads = 256;
+constexpr long long kMaxWgs = kMaxThreads / kThreads;   // of a launch (HIP counts threads modulo 2^32)
 
 // what becomes of a product on its way to memory
 struct Epilogue {
@@ -62,7 +63,7 @@ struct LayOut {
   long long rows, ld, plane;   // plane: elements between planes
   int n, to_ld, blocks_n, blocks, panels;   // panels: [to_ld/32][rows][32]
 };
-struct LayOutArgs { LayOut m[2]; };
+struct LayOutArgs { LayOut m[2]; int first; };   // first: the launch's first block
 // split_check, and for NaN: what two parts leave of a value that is not finite or rounds to infinity
 __device__ inline void parts_check(const f32x4 &v, unsigned long long &missed) {
 #pragma unroll
@@ -75,9 +76,9 @@ __device__ inline void parts_check(const f32x4 &v, unsigned long long &missed) {
 template <int NP>
 __global__ __launch_bounds__(kThreads) void lay_out_kernel(LayOutArgs a) {
   using T = std::conditional_t<NP == 3, float, __bf16>;
-  const int second = (int)blockIdx.x >= a.m[0].blocks;
+  const int at = a.first + (int)blockIdx.x, second = at >= a.m[0].blocks;
   const LayOut &m = a.m[second];
-  const int b = blockIdx.x - (second ? a.m[0].blocks : 0);
+  const int b = at - (second ? a.m[0].blocks : 0);
   const int bi = b / m.blocks_n, bj = b - bi * m.blocks_n;
   const int c = bj * 64 + (threadIdx.x & 7) * 8;
   unsigned long long missed = 0;
@@ -1041,6 +1042,7 @@ Plan plan_tiles(int np, long long I, long long J, long long R) {
   for (int size = 0; size < kSizes; ++size) {
     const TileCost &c = kTiles[np == 3][size];
     const long long tiles = ((I + c.bm - 1) / c.bm) * ((J + c.bn - 1) / c.bn);
+    if (tiles > kMaxWgs && size > 0) continue;   // (of the largest: layout_of refuses the call)
     for (const int want : {1, 2, 3, 4, 6, 8, 12, 16, 24, 32}) {
       if (want > 1 && (want > steps / 4 || tiles * want > 2 * c.fit)) break;
       const long long per = (steps + want - 1) / want, splits = (steps + per - 1) / per, wgs = tiles * splits;
@@ -1069,7 +1071,7 @@ struct Layout {
   Operand a, b;
   int np;
   Plan plan;
-  int64_t part_at, sums_at, bytes;
+  int64_t part_at, sums_at, bytes;   // bytes: -1 of a call with more workgroups than a launch takes (2^40 outputs and more)
   int sum_parts;
 };
 int64_t align256(int64_t n) { return (n + 255) & ~(int64_t)255; }
@@ -1114,7 +1116,8 @@ Layout layout_of(const LinearShape &s, int dt, int op) {
     l.sum_parts = dt == DT_F32 ? (int)((s.M + 63) / 64) : (int)((J + l.plan.bn - 1) / l.plan.bn) * l.plan.splits * 2;
     at += align256((int64_t)l.sum_parts * s.N * 4);
   }
-  l.bytes = at;
+  const long long tiles = ((I + l.plan.bm - 1) / l.plan.bm) * ((J + l.plan.bn - 1) / l.plan.bn);
+  l.bytes = tiles > kMaxWgs || blocks64(l.a.rows, l.a.n) + blocks64(l.b.rows, l.b.n) > 0x7fffffff ? -1 : at;
   return l;
 }
 
@@ -1123,7 +1126,6 @@ template <typename O, bool AR, bool BR, int NP, int BM, int BN, int BK, int STAG
   t.tiles_j = (t.J + BN - 1) / BN;
   t.group = 8;
   const long long wgs = (long long)t.tiles_i * t.tiles_j * t.splits;
-  if (wgs > 0x7fffffffLL) return set_error(RESIST_ESHAPE, "linear: too many outputs");
   gemm_tile_kernel<O, AR, BR, NP, BM, BN, BK, STAGES, WGS><<<(unsigned)wgs, kThreads, 0, st>>>(t);
   RESIST_CHECK_LAUNCH("linear");
   return RESIST_OK;
@@ -1131,7 +1133,7 @@ template <typename O, bool AR, bool BR, int NP, int BM, int BN, int BK, int STAG
 
 template <typename O> int join(const JoinArgs &j, hipStream_t st) {
   const long long wgs = j.sum_wgs + (j.splits > 1 ? (j.I * ((j.J + 7) / 8) + kThreads - 1) / kThreads : 0);
-  if (wgs > 0x7fffffffLL) return set_error(RESIST_ESHAPE, "linear: too many outputs");
+  if (wgs > kMaxWgs) return set_error(RESIST_ESHAPE, "linear: too many outputs");
   prof::Scope sc("linear_join", 0., j.splits > 1 ? (double)j.splits * j.I * j.J * 4 : 0., st);
   gemm_join_kernel<O><<<(unsigned)wgs, kThreads, 0, st>>>(j);
   RESIST_CHECK_LAUNCH("linear_join");
@@ -1142,7 +1144,6 @@ template <typename O> int join(const JoinArgs &j, hipStream_t st) {
 template <typename O, int NP, bool AR, bool BR>
 int product(const Layout &l, const void *a, const void *b, long long I, int J, long long R, const Epilogue &e, float *db, void *work, const char *name,
             double flops, double bytes, hipStream_t st) {
-  if (blocks64(l.a.rows, l.a.n) + blocks64(l.b.rows, l.b.n) > 0x7fffffff) return set_error(RESIST_ESHAPE, "linear: too many rows and columns");
   char *ws = static_cast<char *>(work);
   float *sums = db ? reinterpret_cast<float *>(ws + l.sums_at) : nullptr;
   if (l.a.moved || l.b.moved) {
@@ -1159,10 +1160,13 @@ int product(const Layout &l, const void *a, const void *b, long long I, int J, l
     };
     add(l.a, a, NP == 3 ? sums : nullptr);
     add(l.b, b, nullptr);
-    const long long wgs = (long long)args.m[0].blocks + args.m[1].blocks;
+    const long long blocks = (long long)args.m[0].blocks + args.m[1].blocks;
     prof::Scope sc("linear_lay_out", 0., moved, st);
-    lay_out_kernel<NP><<<(unsigned)wgs, kThreads, 0, st>>>(args);
-    RESIST_CHECK_LAUNCH("linear_lay_out");
+    for (long long first = 0; first < blocks; first += kMaxWgs) {
+      args.first = (int)first;
+      lay_out_kernel<NP><<<(unsigned)std::min(kMaxWgs, blocks - first), kThreads, 0, st>>>(args);
+      RESIST_CHECK_LAUNCH("linear_lay_out");
+    }
   }
   TileArgs t{};
   t.a = reinterpret_cast<const __bf16 *>(l.a.moved ? ws + l.a.at : static_cast<const char *>(a));

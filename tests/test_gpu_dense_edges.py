@@ -104,3 +104,46 @@ def test_layernorm_of_many_rows(m, n):
         part = x[i:i + step].float()
         assert ((mean[i:i + step] - part.mean(1)).abs() <= 100 * U * part.abs().mean(1)).all(), i
         assert (y[i:i + step].float().mean(1).abs() <= 2.0 ** -8).all(), i
+
+
+def test_dense_layers_of_many_rows():
+    """Rows for more workgroups of 64 than one launch takes, laid out (five and three elements a row) and multiplied."""
+    m, k, n, p = (1 << 30) + 3, 5, 3, 0.25
+    x, w = random(m, k, "bf16", 2), random(n, k, "bf16", 3)
+    rng = torch.tensor([3, 5], dtype=torch.int64, device="cuda")
+    at = rows_of(m)
+    kept = np.concatenate([D.kept((3, 5 + i * 2), 1, n, p) for i in at])
+    y = R.linear_forward(x, w, act="relu", p=p, rng=rng)
+    z = host(x[at]) @ host(w).T
+    e = (4 * np.sqrt(k) + 4) * U * (np.abs(host(x[at])) @ np.abs(host(w)).T)
+    want = np.where(kept, np.maximum(z, 0) / (1 - p), 0.0)
+    near(y[at], want, (1.2 * e / (1 - p) + (4 * U + HALF["bf16"] * 1.01) * np.abs(want)) + 1e-38, "forward, sampled")
+    step = 1 << 26
+    wf = w.float()
+    y = R.linear_forward(x, w)
+    for i in range(0, m, step):
+        part, got = x[i:i + step].float(), y[i:i + step].float()
+        for j in range(n):     # a sum of five products: 13 roundings of the sum of magnitudes, on either side
+            terms = part * wf[j]
+            assert ((got[:, j] - terms.sum(1)).abs() <= 26 * U * terms.abs().sum(1) + HALF["bf16"] * 1.01 * terms.sum(1).abs()).all(), (i, j)
+    # y is as good a gradient as any; dx = y w
+    dx = R.linear_dgrad(y, w)
+    for i in range(0, m, step):
+        part, got = y[i:i + step].float(), dx[i:i + step].float()
+        for j in range(k):
+            terms = part * wf[:, j]
+            assert ((got[:, j] - terms.sum(1)).abs() <= 26 * U * terms.abs().sum(1) + HALF["bf16"] * 1.01 * terms.sum(1).abs()).all(), (i, j)
+    del dx
+    dw, db = R.linear_wgrad(y, x)
+    sums = torch.zeros(4, n, k, dtype=torch.float64, device="cuda")
+    for i in range(0, m, step):
+        a, b = y[i:i + step].double(), x[i:i + step].double()
+        for j in range(n):
+            t = a[:, j:j + 1] * b
+            sums[0, j] += t.sum(0)
+            sums[1, j] += t.abs().sum(0)
+            sums[2, j, 0] += a[:, j].sum()
+            sums[3, j, 0] += a[:, j].abs().sum()
+    bound = (4 * np.sqrt(m) + 4) * U
+    near(dw, host(sums[0]), bound * host(sums[1]), "dw")
+    near(db, host(sums[2, :, 0]), bound * host(sums[3, :, 0]), "db")

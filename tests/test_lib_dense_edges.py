@@ -1,0 +1,25 @@
+"""CPU: what the dense operators refuse at the ends of their ranges, and what their binding makes of it, before anything is launched."""
+import ctypes as C
+
+import pytest
+import torch
+
+import paper_2107_00961_amd as R
+from paper_2107_00961_amd import binding as B
+
+P = 256   # an aligned address that nothing reads
+ESHAPE = -2
+
+
+@pytest.mark.parametrize("dt", [0, 1])
+@pytest.mark.parametrize("op,m,k,n", [(0, (1 << 31) - 1, 8, 1 << 20), (1, (1 << 31) - 1, 1 << 20, 8), (2, 1000, 1 << 20, 1 << 20)])
+def test_more_tiles_than_a_launch_takes_are_refused(op, m, k, n, dt):
+    """2^24 workgroups of 256 threads are 2^32, which a launch counts modulo 2^32."""
+    sh, size, L = B._LinearShape(m, k, n, 0, 0, dt), C.c_int64(), R.lib()
+    assert L.resist_linear_workspace_bytes(C.byref(sh), op, C.byref(size)) == ESHAPE
+    call = (L.resist_linear_forward, L.resist_linear_dgrad, L.resist_linear_wgrad)[op]
+    last = (None, P, P, 1 << 62, None) if op < 2 else (P, P, P, 1 << 62, None)
+    assert call(C.byref(sh), P, P, *last) == ESHAPE
+    sh.M = 1 << 20 if op < 2 else 0      # as many as the card could hold
+    sh.N, sh.K = min(n, 4096), min(k, 4096)
+    assert L.resist_linear_workspace_bytes(C.byref(sh), op, C.byref(size)) == 0
