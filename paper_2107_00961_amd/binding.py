@@ -477,8 +477,8 @@ def stem_conv2d_wgrad(dy, x, w_shape, stride, pad, stream=None):
 
 # ---- operators of a dense residual block ---------------------------------------------------------------------------
 # Matrices are two-dimensional tensors [rows, N].  Their rows may be apart (a slice of a wider matrix); one whose rows are not
-# contiguous or not 16-byte aligned at the start is copied first.  Results are new tensors, allocated for the stream the call runs on:
-# the current one, or `stream`.
+# contiguous, not 16-byte aligned at the start, or farther apart than the call takes (2^20 elements for dense layers) is copied
+# first.  Results are new tensors, allocated for the stream the call runs on: the current one, or `stream`.
 ACTIVATIONS = {"none": 0, "relu": 1, "gelu": 2, "gelu_tanh": 3, "silu": 4}
 torch = None     # and what the calls below need of it, from the first of them on: most take less time than torch.cuda.current_stream()
 _DTYPES = {}     # torch dtype -> code
@@ -531,7 +531,10 @@ def _dtype_of(t):
     return code
 
 
-def _matrix(t, what, like=None, shape=None):
+_FAR, _FAR_LINEAR = 1 << 40, 1 << 20    # the largest row strides that the library takes
+
+
+def _matrix(t, what, like=None, shape=None, far=_FAR):
     """t as rows the library takes; checked against the call's first tensor."""
     if t.dim() != 2:
         raise ResistError(f"{what}: a matrix [rows, N] is needed, got {tuple(t.shape)}")
@@ -544,7 +547,7 @@ def _matrix(t, what, like=None, shape=None):
         raise ResistError(f"{what}: rows without elements")
     if t.is_contiguous():
         return t if t.data_ptr() % 16 == 0 else t.clone()
-    if t.stride(1) != 1 and n > 1 or t.stride(0) < n and m > 1 or t.data_ptr() % 16:
+    if t.stride(1) != 1 and n > 1 or not n <= t.stride(0) <= far and m > 1 or t.data_ptr() % 16:
         t = t.contiguous()
     return t
 
@@ -696,12 +699,12 @@ def linear_forward(x, w, bias=None, act="none", p=0.0, rng=None, residual=None, 
     if st is None:
         return _there(linear_forward, stream, x, w, bias, act, p, rng, residual, keep_z)
     dt, code = _dtype_of(x), _activation(act)
-    x = _matrix(x, "x")
+    x = _matrix(x, "x", far=_FAR_LINEAR)
     M, K = x.shape
     w = _weights(w, x, K=K)
     N = w.shape[0]
     bias = _vector(bias, "bias", N, x)
-    residual = _matrix(residual, "residual", x, (M, N)) if residual is not None else None
+    residual = _matrix(residual, "residual", x, (M, N), _FAR_LINEAR) if residual is not None else None
     y = x.new_empty((M, N))
     z = x.new_empty((M, N)) if keep_z else None
     ldx = _ld(x)
@@ -719,13 +722,13 @@ def linear_dgrad(dz, w, act="none", z=None, p=0.0, rng=None, stream=None):
     if st is None:
         return _there(linear_dgrad, stream, dz, w, act, z, p, rng)
     dt, code = _dtype_of(dz), _activation(act)
-    dz = _matrix(dz, "dz")
+    dz = _matrix(dz, "dz", far=_FAR_LINEAR)
     M, N = dz.shape
     w = _weights(w, dz, N=N)
     K = w.shape[1]
     if code and z is None:
         raise ResistError("z: needed for the gradient of an activation")
-    z = _matrix(z, "z", dz, (M, K)) if code else None
+    z = _matrix(z, "z", dz, (M, K), _FAR_LINEAR) if code else None
     dx = dz.new_empty((M, K))
     ldy = _ld(dz)
     ws, n = _linear_ws(dz, 1, M, K, N, 0, ldy, dt)
@@ -740,9 +743,9 @@ def linear_wgrad(dz, x, stream=None):
     if st is None:
         return _there(linear_wgrad, stream, dz, x)
     dt = _dtype_of(dz)
-    dz = _matrix(dz, "dz")
+    dz = _matrix(dz, "dz", far=_FAR_LINEAR)
     M, N = dz.shape
-    x = _matrix(x, "x", dz)
+    x = _matrix(x, "x", dz, far=_FAR_LINEAR)
     if x.shape[0] != M:
         raise ResistError(f"x: {x.shape[0]} rows beside {M} of dz")
     K = x.shape[1]

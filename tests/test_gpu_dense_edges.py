@@ -147,3 +147,25 @@ def test_dense_layers_of_many_rows():
     bound = (4 * np.sqrt(m) + 4) * U
     near(dw, host(sums[0]), bound * host(sums[1]), "dw")
     near(db, host(sums[2, :, 0]), bound * host(sums[3, :, 0]), "db")
+
+
+@pytest.mark.parametrize("dt", ["f32", "bf16"])
+@pytest.mark.parametrize("m", [3, 70])
+def test_dense_layers_on_rows_far_apart(m, dt):
+    """The last token of every sequence of a batch is such a view: rows more than 2^20 elements apart, which the library does not take itself."""
+    k, n, far = 40, 24, (1 << 20) + 16
+
+    def apart(cols, seed):
+        t = torch.full((m, far), float("nan"), device="cuda", dtype=DT[dt])
+        t[:, :cols] = random(m, cols, dt, seed)
+        return t[:, :cols], t[:, :cols].contiguous()
+
+    (x, xc), (dz, dzc), (z, zc), (res, resc) = apart(k, 1), apart(n, 2), apart(k, 3), apart(n, 4)
+    w = random(n, k, dt, 5)
+    assert torch.equal(R.linear_forward(x, w, residual=res), R.linear_forward(xc, w, residual=resc))
+    assert torch.equal(R.linear_dgrad(dz, w, act="gelu", z=z), R.linear_dgrad(dzc, w, act="gelu", z=zc))
+    assert all(torch.equal(a, b) for a, b in zip(R.linear_wgrad(dz, x), R.linear_wgrad(dzc, xc)))
+    # the operators on rows alone take them as they are
+    assert torch.equal(R.layernorm_forward(x)[0], R.layernorm_forward(xc)[0])
+    rng = torch.tensor([1, 2], dtype=torch.int64, device="cuda")
+    assert torch.equal(R.dropout_forward(x, 0.5, rng, residual=z), R.dropout_forward(xc, 0.5, rng, residual=zc))

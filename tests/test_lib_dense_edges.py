@@ -23,3 +23,12 @@ def test_more_tiles_than_a_launch_takes_are_refused(op, m, k, n, dt):
     sh.M = 1 << 20 if op < 2 else 0      # as many as the card could hold
     sh.N, sh.K = min(n, 4096), min(k, 4096)
     assert L.resist_linear_workspace_bytes(C.byref(sh), op, C.byref(size)) == 0
+
+
+def test_rows_farther_apart_than_dense_layers_take_are_copied():
+    for far, copied in (((1 << 20) + 16, True), (1 << 20, False)):
+        v = torch.zeros(3, far)[:, :40]
+        assert (B._matrix(v, "x", far=B._FAR_LINEAR).data_ptr() != v.data_ptr()) == copied
+        assert B._ld(B._matrix(v, "x", far=B._FAR_LINEAR)) == (40 if copied else far)
+        assert B._matrix(v, "x").data_ptr() == v.data_ptr()                                     # the operators on rows alone take them
+        assert B._matrix(v[:1], "x", far=B._FAR_LINEAR).data_ptr() == v.data_ptr()              # one row has no next one
