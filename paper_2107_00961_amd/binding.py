@@ -532,6 +532,7 @@ def _dtype_of(t):
 
 
 _FAR, _FAR_LINEAR = 1 << 40, 1 << 20    # the largest row strides that the library takes
+_MOST = (1 << 31) - 1                    # ctypes would take a larger width modulo 2^32
 
 
 def _matrix(t, what, like=None, shape=None, far=_FAR):
@@ -545,6 +546,8 @@ def _matrix(t, what, like=None, shape=None, far=_FAR):
         raise ResistError(f"{what}: shape {(m, n)} where {shape} is needed")
     if n == 0:
         raise ResistError(f"{what}: rows without elements")
+    if n > _MOST:
+        raise ResistError(f"{what}: rows of {n} elements")
     if t.is_contiguous():
         return t if t.data_ptr() % 16 == 0 else t.clone()
     if t.stride(1) != 1 and n > 1 or not n <= t.stride(0) <= far and m > 1 or t.data_ptr() % 16:
@@ -688,6 +691,8 @@ def _linear_ws(like, op, *shape):
 def _weights(w, like, K=None, N=None):
     if w.dim() != 2 or K is not None and w.shape[1] != K or N is not None and w.shape[0] != N or w.shape[0] < 1:
         raise ResistError(f"w: [N, K] is needed, got {tuple(w.shape)} beside {tuple(like.shape)}")
+    if w.shape[0] > _MOST:
+        raise ResistError(f"w: {w.shape[0]} rows")
     w = _matrix(w, "w", like)
     return w if w.is_contiguous() else w.contiguous()
 

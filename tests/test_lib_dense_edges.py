@@ -32,3 +32,14 @@ def test_rows_farther_apart_than_dense_layers_take_are_copied():
         assert B._ld(B._matrix(v, "x", far=B._FAR_LINEAR)) == (40 if copied else far)
         assert B._matrix(v, "x").data_ptr() == v.data_ptr()                                     # the operators on rows alone take them
         assert B._matrix(v[:1], "x", far=B._FAR_LINEAR).data_ptr() == v.data_ptr()              # one row has no next one
+
+
+@pytest.mark.parametrize("n", [1 << 31, (1 << 32) + 8])
+def test_widths_past_32_bits_are_refused(n):
+    """They would reach the library as what is left of them modulo 2^32."""
+    wide, tall = torch.empty(4, n, device="meta"), torch.empty(n, 4, device="meta")
+    with pytest.raises(R.ResistError, match=f"rows of {n} elements"):
+        B._matrix(wide, "x")
+    with pytest.raises(R.ResistError, match=f"w: {n} rows"):
+        B._weights(tall, torch.empty(4, 4, device="meta"), K=4)
+    assert B._matrix(tall, "x").shape == (n, 4)      # rows are counted in 64 bits, and the library's to refuse
