@@ -488,11 +488,12 @@ _F32 = _raw_stream = _device = None
 
 def _start():
     global torch, _F32, _INT64, _raw_stream, _device
-    import torch
-    _F32, _INT64 = torch.float32, (torch.int64, torch.uint64)
-    _DTYPES.update({torch.float32: 0, torch.bfloat16: 1})
-    _device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
-    _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", lambda i: torch.cuda.current_stream(i).cuda_stream)
+    import torch as found
+    _F32, _INT64 = found.float32, (found.int64, found.uint64)
+    _DTYPES.update({found.float32: 0, found.bfloat16: 1})
+    _device = getattr(found._C, "_cuda_getDevice", found.cuda.current_device)
+    _raw_stream = getattr(found._C, "_cuda_getCurrentRawStream", lambda i: found.cuda.current_stream(i).cuda_stream)
+    torch = found    # last: another thread's first call takes its being there for that of the others
 
 
 def _on(t, stream):

@@ -43,3 +43,19 @@ def test_widths_past_32_bits_are_refused(n):
     with pytest.raises(R.ResistError, match=f"w: {n} rows"):
         B._weights(tall, torch.empty(4, 4, device="meta"), K=4)
     assert B._matrix(tall, "x").shape == (n, 4)      # rows are counted in 64 bits, and the library's to refuse
+
+
+def test_first_calls_of_two_threads(monkeypatch):
+    """Whoever finds torch in its place finds everything else that the calls need: it is bound last."""
+    seen = []
+
+    class Watched(dict):
+        def update(self, *a):
+            seen.append(B.torch)
+            dict.update(self, *a)
+
+    for name, value in (("torch", None), ("_F32", None), ("_INT64", ()), ("_raw_stream", None), ("_device", None), ("_DTYPES", Watched())):
+        monkeypatch.setattr(B, name, value)
+    B._start()
+    assert seen == [None]
+    assert B.torch is torch and B._F32 is torch.float32 and B._INT64 and B._raw_stream and B._device and B._DTYPES[torch.bfloat16] == 1
