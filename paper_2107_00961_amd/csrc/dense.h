@@ -90,6 +90,9 @@ __device__ inline void raw_load(const __bf16 *p, int left, Raw8<__bf16> &r) {
     for (int e = 0; e < 4; ++e) r.a[e] = t[2 * e] | (unsigned)t[2 * e + 1] << 16;
   }
 }
+// what was requested is there from here on
+__device__ inline void arrived(Raw8<float> &r) { asm volatile("" : "+v"(r.a), "+v"(r.b)); }
+__device__ inline void arrived(Raw8<__bf16> &r) { asm volatile("" : "+v"(r.a)); }
 __device__ inline void widen(const Raw8<float> &r, float (&v)[8]) {
 #pragma unroll
   for (int e = 0; e < 4; ++e) { v[e] = r.a[e]; v[e + 4] = r.b[e]; }

@@ -245,6 +245,8 @@ __global__ __launch_bounds__(threads_of(TPR)) void ln_bwd_kernel(LnArgs a) {
         widen(rx[i], h[i]);
         widen(rdy[i], g[i]);
         add[i] = rad[i];
+        // where dx takes the addend's place, another thread may store into a vector that overlaps this one once the row's sums are joined
+        if (decltype(masked)::value && a.addend) arrived(add[i]);
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
           h[i][e] = (h[i][e] - mu) * rs;

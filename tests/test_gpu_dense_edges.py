@@ -169,3 +169,30 @@ def test_dense_layers_on_rows_far_apart(m, dt):
     assert torch.equal(R.layernorm_forward(x)[0], R.layernorm_forward(xc)[0])
     rng = torch.tensor([1, 2], dtype=torch.int64, device="cuda")
     assert torch.equal(R.dropout_forward(x, 0.5, rng, residual=z), R.dropout_forward(xc, 0.5, rng, residual=zc))
+
+
+# ---- layer norm in place ----------------------------------------------------------------------------------------------
+@pytest.mark.parametrize("dt", ["f32", "bf16"])
+@pytest.mark.parametrize("n", [7, 100, 1001, 1100, 2049, 4100, 8190, 8200])
+def test_layernorm_in_place(n, dt):
+    """y over x, and dx over dy, x and the addend: what results of their own hold.  Where a row is no whole number of vectors, the last one overlaps the one
+    before, another thread's and beyond 1024 another wave's.  Workgroups take several rows one after the other."""
+    m, code, L, st = 2500, {"f32": 0, "bf16": 1}[dt], R.lib(), torch.cuda.current_stream().cuda_stream
+    x, dy, add = (random(m, n, dt, s) for s in (1, 2, 3))
+    gamma = 1 + 0.1 * random(1, n, "f32", 4)[0].contiguous()
+    want, mean, rstd = R.layernorm_forward(x, gamma)
+    t, stat = x.clone(), torch.empty(2, m + 4, device="cuda")
+    assert L.resist_layernorm_forward(m, n, code, t.data_ptr(), 0, gamma.data_ptr(), None, 1e-5, t.data_ptr(), 0, stat[0].data_ptr(), stat[1].data_ptr(), st) == 0
+    assert torch.equal(t, want) and torch.equal(stat[0, :m], mean) and torch.equal(stat[1, :m], rstd)
+    size = C.c_int64()
+    assert L.resist_layernorm_workspace_bytes(m, n, C.byref(size)) == 0
+    ws = torch.empty(size.value, dtype=torch.uint8, device="cuda")
+    for addend in (None, add):
+        want, dgamma, dbeta = R.layernorm_backward(dy, x, gamma, mean, rstd, addend=addend)
+        for k in range(2 if addend is None else 3):
+            t = [dy.clone(), x.clone(), None if addend is None else addend.clone()]
+            dg, db = torch.empty(n, device="cuda"), torch.empty(n, device="cuda")
+            assert L.resist_layernorm_backward(m, n, code, t[0].data_ptr(), 0, t[1].data_ptr(), 0, gamma.data_ptr(), mean.data_ptr(), rstd.data_ptr(),
+                                               None if addend is None else t[2].data_ptr(), 0, t[k].data_ptr(), 0, dg.data_ptr(), db.data_ptr(), ws.data_ptr(),
+                                               size.value, st) == 0
+            assert torch.equal(t[k], want) and torch.equal(dg, dgamma) and torch.equal(db, dbeta), (k, addend is None)
