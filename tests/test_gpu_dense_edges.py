@@ -196,3 +196,55 @@ def test_layernorm_in_place(n, dt):
                                                None if addend is None else t[2].data_ptr(), 0, t[k].data_ptr(), 0, dg.data_ptr(), db.data_ptr(), ws.data_ptr(),
                                                size.value, st) == 0
             assert torch.equal(t[k], want) and torch.equal(dg, dgamma) and torch.equal(db, dbeta), (k, addend is None)
+
+
+# ---- a block's gradients ----------------------------------------------------------------------------------------------
+@pytest.mark.parametrize("dt", ["f32", "bf16"])
+@pytest.mark.parametrize("act", ["relu", "gelu", "silu"])
+def test_gradients_of_a_block_from_what_it_kept(act, dt):
+    """Every operator of the backward pass against the oracle's of the very tensors it was given (what the forward pass kept, the gradients on the way as
+    stored), so that no ReLU is on another side of 0 and every element has its own bound: sums of n terms 4 sqrt(n) + 4 roundings
+    of the sum of magnitudes, a slope 16 max(1, |z|), a stored value half a step."""
+    m, n, hidden, p = 260, 200, 520, 0.2
+    x, dy, w1, w2 = random(m, n, dt, 1), random(m, n, dt, 2), random(hidden, n, dt, 3) / n ** 0.5, random(n, hidden, dt, 4) / hidden ** 0.5
+    gamma, beta, b1, b2 = 1 + 0.1 * random(1, n, "f32", 5)[0], 0.1 * random(1, n, "f32", 6)[0], 0.1 * random(1, hidden, "f32", 7)[0], 0.1 * random(1, n, "f32", 8)[0]
+    r1, r2 = (7, 0), (7, 1 << 33)
+    rng1, rng2 = (torch.tensor(r, dtype=torch.int64, device="cuda") for r in (r1, r2))
+    nx, mean, rstd = R.layernorm_forward(x, gamma, beta)
+    h, z1 = R.linear_forward(nx, w1, b1, act=act, p=p, rng=rng1, keep_z=True)
+    y = R.linear_forward(h, w2, b2, p=p, rng=rng2, residual=x)
+
+    def terms(a, b, k):
+        return (4 * np.sqrt(k) + 4) * U * (np.abs(a) @ np.abs(b))
+
+    half = HALF[dt] * 1.01
+    z64, _ = D.linear(host(nx), host(w1), host(b1))
+    near(z1, z64, terms(host(nx), host(w1).T, n) + (2 * U + half) * np.abs(z64) + 1e-38, "z1")
+    want = D.dropout(D.act(z64, act), p, r1)
+    near(h, want, (1.2 * terms(host(nx), host(w1).T, n) + 16 * U * np.abs(z64)) / (1 - p) * D.kept(r1, m, hidden, p) + (6 * U + half) * np.abs(want) + 1e-38, "h")
+    want, _ = D.linear(host(h), host(w2), host(b2), "none", p, r2, host(x))
+    near(y, want, terms(host(h), host(w2).T, hidden) / (1 - p) + 8 * U * np.abs(want - host(x)) + (U + half) * np.abs(want) + 1e-38, "y")
+
+    dz2 = R.dropout_backward(dy, p, rng2)
+    want = D.dropout(host(dy), p, r2)
+    near(dz2, want, (4 * U + half) * np.abs(want) + 1e-45, "dz2")
+    dz1 = R.linear_dgrad(dz2, w2, act=act, z=z1, p=p, rng=rng1)
+    v = D.dropout(host(dz2) @ host(w2), p, r1)
+    want = v * D.slope(host(z1), act)
+    near(dz1, want, 1.2 * terms(host(dz2), host(w2), n) / (1 - p) * D.kept(r1, m, hidden, p) * ((act != "relu") + (act == "relu") * (want != 0))
+         + np.abs(v) * 16 * U * np.maximum(1, np.abs(host(z1))) * (act != "relu") + (4 * U + half) * np.abs(want) + 1e-38, "dz1")
+    for name, g, a in (("2", dz2, h), ("1", dz1, nx)):
+        dw, db = R.linear_wgrad(g, a)
+        near(dw, host(g).T @ host(a), terms(host(g).T, host(a), m) + 1e-38, "dw" + name)
+        near(db, host(g).sum(0), (4 * np.sqrt(m) + 4) * U * np.abs(host(g)).sum(0) + 1e-38, "db" + name)
+    dn = R.linear_dgrad(dz1, w1)
+    want = host(dz1) @ host(w1)
+    near(dn, want, terms(host(dz1), host(w1), hidden) + (2 * U + half) * np.abs(want) + 1e-38, "dn")
+    dx, dgamma, dbeta = R.layernorm_backward(dn, x, gamma, mean, rstd, addend=dy)
+    args = host(dn), host(x), host(gamma), host(mean), host(rstd)
+    want, dg, db = D.layernorm_backward(*args, host(dy))
+    xhat, g = np.abs(host(x) - host(mean)[:, None]) * host(rstd)[:, None], np.abs(host(dn) * host(gamma))
+    s1, s2 = g.mean(1, keepdims=True), (g * xhat).mean(1, keepdims=True)
+    near(dx, want, host(rstd)[:, None] * (8 * U * (g + s1 + xhat * s2) + 54 * U * (s1 + xhat * s2)) + 2 * U * np.abs(host(dy)) + (2 * U + half) * np.abs(want) + 1e-38, "dx")
+    near(dgamma, dg, (m / 128 + 12) * U * (np.abs(host(dn)) * xhat).sum(0) + 1e-38, "dgamma")
+    near(dbeta, db, (m / 128 + 12) * U * np.abs(host(dn)).sum(0) + 1e-38, "dbeta")
