@@ -994,13 +994,19 @@ __global__ __launch_bounds__(kThreads) void few_rows_wgrad_kernel(const T *dz, l
 }
 
 // ---- plans ----------------------------------------------------------------------------------------------------------
-// Up to this many rows go without tiles.  us, 4096 -> 4096, tiles (with what they lay out and join) -> few rows:
+// Up to this many rows go without tiles; a bf16 forward pass of more than 16 rows does while its weights are few (fewer of odd length, whose rows start anywhere).
+// us, 4096 -> 4096, tiles (with what they lay out and join) -> few rows:
 //   fp32 1 row: forward 50 -> 15, data gradient 53 -> 16, weight gradient 33 -> 13      17 rows: 50 -> 20, 55 -> 20, 34 (tiles)
 //   fp32 64 rows: 51 -> 39, 55 -> 41     bf16 1 row: forward 11.6 -> 7.4 (4.5 TB/s), data gradient 11 (tiles; 40 with 64 columns to a workgroup), weight gradient 23 -> 13.4 (5 TB/s)
-//   bf16 16 rows: forward 12.5 -> 10.1, weight gradient 24 -> 16.5     32 rows: forward 13.2 -> 14.1, at 512 -> 512 5.4 -> 4.5
-int few(int dt, int op) {
+//   bf16 16 rows: forward 12.5 -> 10.1, weight gradient 24 -> 16.5
+// bf16 forward, 17 | 32 rows, tiles -> few rows:  512 -> 512 5.8 -> 3.7 | 5.8 -> 4.0     1024 -> 4096 8.6 -> 5.6 | 8.7 -> 6.4     2048 -> 2048 9.6 -> 8.0 | 9.8 -> 9.4
+//   2048 -> 8192 12.3 -> 12.9 | 12.6 -> 15.9     4096 -> 4096 12.3 -> 13.7 | 12.6 -> 16.2     8192 -> 2048 13.6 -> 23.0 | 13.7 -> 27.6
+//   511 -> 512 9.6 -> 7.3 | 9.6 -> 8.8     1023 -> 1024 11.7 -> 10.9 | 11.7 -> 13.7     2047 -> 1024 13.5 -> 17.2 | 13.6 -> 22.7
+int few(const LinearShape &s, int dt, int op) {
   if (op == 2) return 16;
-  return dt == DT_F32 ? 64 : op == 0 ? 32 : 0;
+  if (dt == DT_F32) return 64;
+  if (op == 1) return 0;
+  return (int64_t)s.K * s.N <= (s.K % 2 ? 1 << 19 : 1 << 22) ? 32 : 16;
 }
 // Ranges of the reduction: a few hundred workgroups where there are less than one for every other CU, as long as each wave has whole turns of loads.
 struct FewPlan { int wgs, splits, per; };
@@ -1233,7 +1239,7 @@ double bytes_of(const LinearShape &s, int dt, double outs) { return ((double)s.M
 
 int64_t linear_workspace(const LinearShape &s, int dt, int op) {
   if (s.M == 0) return 0;
-  if (s.M <= few(dt, op)) {
+  if (s.M <= few(s, dt, op)) {
     if (op == 2) return 0;
     const int J = op == 0 ? s.N : s.K;
     const FewPlan p = plan_few(dt, op, s.M, J, op == 0 ? s.K : s.N);
@@ -1248,7 +1254,7 @@ int linear_fwd(const LinearShape &s, int dt, const void *x, const void *w, const
   e.out = y; e.ldo = s.ldy; e.bias = le.bias; e.z_out = le.z; e.ldz = le.ldz; e.res = le.residual; e.ldr = le.ldr; e.act = le.act;
   e.d = make_dropout(le.drop); e.words = (s.N + 1) / 2;
   const double bytes = bytes_of(s, dt, (double)s.M * s.N * esize(dt) * ((le.z != nullptr) + (le.residual != nullptr)));
-  if (s.M <= few(dt, 0)) return few_rows(s, dt, 0, x, s.ldx, w, e, work, "linear_few_rows_fwd", bytes, st);
+  if (s.M <= few(s, dt, 0)) return few_rows(s, dt, 0, x, s.ldx, w, e, work, "linear_few_rows_fwd", bytes, st);
   const Layout l = layout_of(s, dt, 0);
   return dt == DT_F32 ? product<float, 3, true, true>(l, x, w, s.M, s.N, s.K, e, nullptr, work, "linear_fwd", flops_of(s), bytes, st)
                       : product<__bf16, 1, true, true>(l, x, w, s.M, s.N, s.K, e, nullptr, work, "linear_fwd", flops_of(s), bytes, st);
@@ -1260,7 +1266,7 @@ int linear_dgrad(const LinearShape &s, int dt, const void *dz, const void *w, co
   e.out = dx; e.ldo = s.ldx; e.z_in = lt.act == RESIST_ACT_NONE ? nullptr : lt.z; e.ldz = lt.ldz; e.act = lt.act;
   e.d = make_dropout(lt.drop); e.words = (s.K + 1) / 2;
   const double bytes = bytes_of(s, dt, e.z_in ? (double)s.M * s.K * esize(dt) : 0.);
-  if (s.M <= few(dt, 1)) return few_rows(s, dt, 1, dz, s.ldy, w, e, work, "linear_few_rows_dgrad", bytes, st);
+  if (s.M <= few(s, dt, 1)) return few_rows(s, dt, 1, dz, s.ldy, w, e, work, "linear_few_rows_dgrad", bytes, st);
   const Layout l = layout_of(s, dt, 1);
   return dt == DT_F32 ? product<float, 3, true, false>(l, dz, w, s.M, s.K, s.N, e, nullptr, work, "linear_dgrad", flops_of(s), bytes, st)
                       : product<__bf16, 1, true, false>(l, dz, w, s.M, s.K, s.N, e, nullptr, work, "linear_dgrad", flops_of(s), bytes, st);
@@ -1268,7 +1274,7 @@ int linear_dgrad(const LinearShape &s, int dt, const void *dz, const void *w, co
 
 int linear_wgrad(const LinearShape &s, int dt, const void *dz, const void *x, float *dw, float *db, void *work, hipStream_t st) {
   const double bytes = ((double)s.M * s.K + (double)s.M * s.N) * esize(dt) + 4. * s.N * s.K;
-  if (s.M <= few(dt, 2)) {
+  if (s.M <= few(s, dt, 2)) {
     const dim3 wgs((s.K + 255) / 256, (s.N + 63) / 64);
     const int M = (int)s.M;
     prof::Scope sc("linear_few_rows_wgrad", flops_of(s), bytes, st);

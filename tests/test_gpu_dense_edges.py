@@ -248,3 +248,16 @@ def test_gradients_of_a_block_from_what_it_kept(act, dt):
     near(dx, want, host(rstd)[:, None] * (8 * U * (g + s1 + xhat * s2) + 54 * U * (s1 + xhat * s2)) + 2 * U * np.abs(host(dy)) + (2 * U + half) * np.abs(want) + 1e-38, "dx")
     near(dgamma, dg, (m / 128 + 12) * U * (np.abs(host(dn)) * xhat).sum(0) + 1e-38, "dgamma")
     near(dbeta, db, (m / 128 + 12) * U * np.abs(host(dn)).sum(0) + 1e-38, "dbeta")
+
+
+@pytest.mark.parametrize("m", [16, 17, 32, 33])
+@pytest.mark.parametrize("k,n", [(2048, 2048), (2056, 2048), (511, 1024), (511, 1030)])
+def test_dense_layers_of_few_rows_and_many_weights(m, k, n):
+    """bf16, on either side of where rows are too many, or weights, to go without tiles."""
+    x, w, res = random(m, k, "bf16", 1), random(n, k, "bf16", 2) / k ** 0.5, random(m, n, "bf16", 3)
+    y, z = R.linear_forward(x, w, act="silu", residual=res, keep_z=True)
+    want = host(x) @ host(w).T
+    e = (4 * np.sqrt(k) + 4) * U * (np.abs(host(x)) @ np.abs(host(w)).T)
+    near(z, want, e + HALF["bf16"] * np.abs(want) + 1e-38, "z")
+    out = D.act(want, "silu") + host(res)
+    near(y, out, 1.2 * e + 16 * U * np.abs(want) + (U + HALF["bf16"]) * np.abs(out) + 1e-38, "y")
