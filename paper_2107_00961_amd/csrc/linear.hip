@@ -228,7 +228,7 @@ __device__ inline void bias_of(const Epilogue &e, int j, int left, float (&b)[8]
 // 16 bytes a lane from a buffer to LDS at `to` and on, in lane order.  Written out because the compiler, which sees that LDS is written, waits for
 // all transfers before the next read of any of it; what is waited for, and where, is wait_and_meet's.
 __device__ inline void transfer(__amdgpu_buffer_rsrc_t r, unsigned off, unsigned to) {
-  asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tbuffer_load_dwordx4 %0, %1, 0 offen lds" ::"v"(off), "s"(r), "s"(to) : "memory");
+  asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tbuffer_load_dwordx4 %0, %1, 0 offen lds" ::"v"(off), "s"(r), "s"(to) : "memory", "m0");
 }
 template <int N> __device__ inline void wait_and_meet() {   // at most N of this wave's transfers to LDS under way, all of its reads done
   asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(N) : "memory");
