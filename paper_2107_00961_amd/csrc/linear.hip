@@ -132,7 +132,7 @@ __global__ __launch_bounds__(kThreads) void lay_out_kernel(LayOutArgs a) {
 // staged element is read from LDS (256x256: 1024 clocks of reading and 512 of arriving for 2048 of products).  Bound by the matrix cores and what
 // the chip's power leaves of its clock: 8192 x 8192 -> 2048 in bf16 192 us (1.43 PFLOP/s, the cores at work in 72 % of 362 thousand clocks at 1.86 GHz),
 // 2000 x 1024 -> 1024 in fp32 30 us beside 8 of laying out.  The epilogue's arithmetic is not hidden, one workgroup having a compute unit to itself: with GELU,
-// dropout and z 8192 x 2048 -> 8192 takes 290 ... 305 us for 213 ... 240 (making the mask between the products, though it fits, saved 1 %).
+// dropout and z 8192 x 2048 -> 8192 takes 290 ... 328 us for 213 ... 240 (making the mask between the products, though it fits, saved 1 %).
 // Layout in LDS.  Lane order leaves no room for padding, so what keeps rows off each other's banks is which 16-byte piece a lane asks for:
 //   reduction contiguous (R): a row is an index i, BK values of r: piece c of row i lies at c ^ f(i), f = (i >> 1) & 7 (BK 64, two rows to 256
 //     bytes), (i >> 2) & 3 (BK 32, four rows): sixteen consecutive rows' pieces c fill the 256 bytes of the 64 banks;
@@ -248,7 +248,8 @@ __device__ inline void tile_of(int bid, int tiles_i, int tiles_j, int group, int
 }
 
 // BM x BN outputs from the operands as they are, in fp32 on its own matrix instruction, 64x64 at a time: for operands and results that three parts do
-// not hold.  `lds`: 18 KB.  to(i, j, v) takes an output.
+// not hold.  Bound by its loads, an element each with two barriers every 32 steps: 2000 x 1024 -> 1024 with one such value in x takes 186 us for 40, 8192 x 2048 -> 2048
+// 1835 for 354 (one tile's time, most of it), with one in every block 3171.  `lds`: 18 KB.  to(i, j, v) takes an output.
 template <bool AR, bool BR, int BM, int BN, typename To>
 __device__ inline void plain_tile(const TileArgs &g, long long i0, int j0, long long rbeg, long long rend, char *lds, To to) {
   constexpr int BK = 32;
