@@ -1042,16 +1042,20 @@ struct Plan {
   int bm, bn, splits;
   long long per_split;
 };
+// Ranges are of 2^18 of the reduction at most: a sum in fp32 that has grown past 2^20 of its terms loses their bits (plain_tile's, a term or two at a time:
+// weight gradients of 2^28 rows in 32 ranges were off by 4e-3 of their magnitude, in 1025 by 2e-5).
+constexpr long long kMostSteps = (1 << 18) / 64;
 Plan plan_tiles(int np, long long I, long long J, long long R) {
-  const long long steps = (R + 63) / 64;
+  const long long steps = (R + 63) / 64, least_splits = (steps + kMostSteps - 1) / kMostSteps;
   Plan best{};
   double least = 0.;
   for (int size = 0; size < kSizes; ++size) {
     const TileCost &c = kTiles[np == 3][size];
     const long long tiles = ((I + c.bm - 1) / c.bm) * ((J + c.bn - 1) / c.bn);
     if (tiles > kMaxWgs && size > 0) continue;   // (of the largest: layout_of refuses the call)
-    for (const int want : {1, 2, 3, 4, 6, 8, 12, 16, 24, 32}) {
-      if (want > 1 && (want > steps / 4 || tiles * want > 2 * c.fit)) break;
+    for (const int some : {1, 2, 3, 4, 6, 8, 12, 16, 24, 32}) {
+      const long long want = std::max<long long>(some, least_splits);
+      if (want > least_splits && (want > steps / 4 || tiles * want > 2 * c.fit)) break;
       const long long per = (steps + want - 1) / want, splits = (steps + per - 1) / per, wgs = tiles * splits;
       const long long rounds = wgs / c.fit, rest = wgs - rounds * c.fit;
       double t = kLaunch + rounds * (c.start + per * c.full);
@@ -1124,7 +1128,7 @@ Layout layout_of(const LinearShape &s, int dt, int op) {
     at += align256((int64_t)l.sum_parts * s.N * 4);
   }
   const long long tiles = ((I + l.plan.bm - 1) / l.plan.bm) * ((J + l.plan.bn - 1) / l.plan.bn);
-  l.bytes = tiles > kMaxWgs || blocks64(l.a.rows, l.a.n) + blocks64(l.b.rows, l.b.n) > 0x7fffffff ? -1 : at;
+  l.bytes = tiles * l.plan.splits > kMaxWgs || blocks64(l.a.rows, l.a.n) + blocks64(l.b.rows, l.b.n) > 0x7fffffff ? -1 : at;
   return l;
 }
 

@@ -261,3 +261,29 @@ def test_dense_layers_of_few_rows_and_many_weights(m, k, n):
     near(z, want, e + HALF["bf16"] * np.abs(want) + 1e-38, "z")
     out = D.act(want, "silu") + host(res)
     near(y, out, 1.2 * e + 16 * U * np.abs(want) + (U + HALF["bf16"]) * np.abs(out) + 1e-38, "y")
+
+
+@pytest.mark.parametrize("dt,small", [("f32", None), ("f32", 1e-35), ("bf16", None)])
+def test_weight_gradient_over_many_rows(dt, small):
+    """Sums of 2^28 terms of one sign, which may not be lost against what the sum has grown to; `small`: with values that three bf16 parts do not hold.
+    Ranges of 2^18 rows are summed on their own, so a sum is as exact as one of 2^18 terms, within 4 sqrt(2^18) + 4 roundings, and their joining, 2^10 more."""
+    m, k, n = (1 << 28) + 5, 8, 3
+    torch.cuda.empty_cache()
+    g = torch.Generator(device="cuda").manual_seed(1)
+    x = torch.empty(m, k, device="cuda").normal_(generator=g).to(DT[dt])
+    dz = x[:, :n].relu()
+    if small:
+        dz[::64, 0] = small
+    dw, db = R.linear_wgrad(dz, x)
+    want, size = torch.zeros(2, n, k, dtype=torch.float64, device="cuda")
+    sums = torch.zeros(n, dtype=torch.float64, device="cuda")
+    for i in range(0, m, 1 << 25):
+        a, b = dz[i:i + (1 << 25)].double(), x[i:i + (1 << 25)].double()
+        sums += a.sum(0)
+        for j in range(n):
+            terms = a[:, j:j + 1] * b
+            want[j] += terms.sum(0)
+            size[j] += terms.abs().sum(0)
+    bound = (4 * 2 ** 9 + 4 + 2 ** 10) * U
+    near(dw, host(want), bound * host(size), "dw")
+    near(db, host(sums), bound * host(sums), "db")
